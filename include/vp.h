@@ -62,6 +62,7 @@ typedef enum vp_mode { VP_MODE_MEAN = 0, VP_MODE_SURROGATE = 1, VP_MODE_FULL = 2
 /* Bits of the device error word. */
 #define VP_DEVERR_WAIT_TIMEOUT 1u   /* an mbarrier wait hit its time limit */
 #define VP_DEVERR_NAN_SALIENCY 2u   /* a saliency was NaN; that head was routed to full */
+#define VP_DEVERR_PAGE 4u           /* a sequence or page id outside the paged cache */
 
 typedef struct vp_dims {
   int32_t N;        /* tokens = views S x tokens per view P, all views at once (Algorithm 1) */
@@ -349,6 +350,114 @@ vp_status vp_router_noalloc(const vp_dims* dims, const vp_bf16* qkv, const vp_ro
    nothing. */
 vp_status vp_router_noalloc_error(uint32_t* host_bits, void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Streaming: views (or any tokens) that arrive over time.  The paper attends over all views at
+ * once; these operators carry the same heads to sequences that grow: new tokens are rotated and
+ * appended to a paged cache of keys and values, and attend over it.
+ *
+ * Several sequences are packed along the token axis: sequence b owns the tokens cu[b] ..
+ * cu[b + 1] - 1 of the T new ones (cu: device int32 [B + 1], ascending, cu[0] = 0, cu[B] <= T;
+ * a sequence may have none).  Query heads come in groups: head h reads kv head h / (Hq / Hkv).
+ *
+ * A new token i of a chunk of n, in a sequence of L tokens after the append (L = n for a prompt),
+ * sees the keys j < lim(i):
+ *   block = 0:  lim = L                                          (no mask inside the chunk)
+ *   block >= 1: lim = L - n + min(n, (i / block + 1) block)
+ * so block = 1 is the ordinary causal mask and block = tokens per view lets every view see
+ * itself and the views before it (views counted from the chunk's start).  A row with lim <= 0
+ * sees nothing: its output is 0 and its log-sum is -infinity.  Keys and values that a row does
+ * not see do not reach its output, whatever they hold (NaN and infinities included).
+ *
+ * Strides are in elements between tokens (a multiple of 8, at least heads x d), so that q, k and v
+ * may be slices of a packed projection [T][Hq + 2 Hkv][d]; heads and channels are contiguous.
+ * Every tensor pointer is 16-byte aligned.  Lengths, offsets and the page table are read on the
+ * device when the kernels run; a length or page id outside the cache is clamped or skipped and
+ * sets VP_DEVERR_PAGE in the workspace's error word.
+ */
+#define VP_DTYPE_BF16 0
+#define VP_DTYPE_FP16 1
+
+typedef struct vp_attn_dims {
+  int32_t Hq;     /* query heads, 1 .. 128, a multiple of Hkv */
+  int32_t Hkv;    /* key / value heads */
+  int32_t d;      /* head dim: 64 or 128 */
+  int32_t dtype;  /* VP_DTYPE_*: of q, k, v, the cache and the output */
+  int32_t block;  /* mask (see above), >= 0 */
+  float scale;    /* factor on q . k (1 / sqrt(d) in the paper's softmax attention); finite */
+} vp_attn_dims;
+
+/* Paged cache: a pool of pages shared by all sequences.  Token j of sequence b lies in page
+   page_table[b][j / page_size], row j % page_size. */
+typedef struct vp_paged_kv {
+  void* k;                     /* [n_pages][Hkv][page_size][d] */
+  void* v;                     /* [n_pages][Hkv][page_size][d] */
+  const int32_t* page_table;   /* [B][table_width] */
+  int32_t n_pages;
+  int32_t page_size;           /* a power of two, 16 .. 1024 */
+  int32_t table_width;         /* pages of a row of the table */
+} vp_paged_kv;
+
+/* Rotary positions.  Pair i < rot_dim / 2 of a head's first rot_dim channels turns by
+   pos x turns[i] of a whole turn, (a, b) -> scale (a cos - b sin, b cos + a sin); the other channels
+   are copied.  turns[i] is a 64-bit fraction of a turn (2^64 = one turn): the product with
+   the position wraps, which reduces the angle exactly at any position.  The table carries the base
+   and any scaling for long contexts. */
+typedef struct vp_rope_options {
+  const int64_t* turns;  /* [rot_dim / 2] device */
+  int32_t rot_dim;       /* 0 (no rotation) or a multiple of 16, at most d */
+  int32_t interleaved;   /* 0: pairs (i, i + rot_dim / 2); 1: pairs (2 i, 2 i + 1) */
+  float scale;           /* factor on the rotated channels (1 but for some long-context scalings) */
+} vp_rope_options;
+
+/* Bytes of workspace that vp_prompt_attention and vp_paged_attention need for up to T packed
+   tokens in up to B sequences (host; writes *bytes). */
+vp_status vp_attn_workspace_size(const vp_attn_dims* dims, int32_t T, int32_t B, size_t* bytes);
+
+/*
+ * vp_rope_append -- rotates the new tokens' q and k and writes k and v behind what the cache
+ * holds of their sequences: token i of a chunk of n goes to slot kv_len[b] - n + i.
+ *   q, k, v    [T][heads][d] with their strides; q NULL: only k and v.
+ *   kv_len     [B] int32: lengths after the append (NULL without kv)
+ *   positions  [T] int32 (>= 0), or NULL: the slot (without kv: the index in the chunk)
+ *   kv         HOST pointer, or NULL: nothing is appended (v may then be NULL)
+ *   q_out      rotated q (may be q itself); NULL only if q is
+ *   k_out      rotated k, packed (may be k itself), or NULL; needed without kv
+ *   ws         workspace whose error word takes VP_DEVERR_PAGE, or NULL
+ * A token whose slot is negative, past the table, or on a page id outside the pool is not
+ * written to the cache.  Two tokens of one call never share a slot unless sequences share pages.
+ */
+vp_status vp_rope_append(const vp_attn_dims* dims, const vp_rope_options* rope, int32_t T, int32_t B,
+                         const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                         const void* v, int64_t v_stride, const int32_t* cu, const int32_t* kv_len,
+                         const int32_t* positions, const vp_paged_kv* kv, void* q_out,
+                         int64_t q_out_stride, void* k_out, int64_t k_out_stride, void* ws,
+                         size_t ws_bytes, void* stream);
+
+/*
+ * vp_prompt_attention -- softmax attention of whole packed prompts over themselves.
+ *   q, k, v  [T][heads][d] with their strides;  out [T][Hq][d], out_stride
+ *   lse      [T][Hq] float or NULL: log of the row's softmax denominator (natural)
+ *   ws       vp_attn_workspace_size bytes, contents arbitrary but for its error word (first 4
+ *            bytes, zero at first)
+ * Tokens past cu[B] are left alone in out and lse.
+ */
+vp_status vp_prompt_attention(const vp_attn_dims* dims, int32_t T, int32_t B, const void* q,
+                              int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                              int64_t v_stride, const int32_t* cu, void* out, int64_t out_stride,
+                              float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * vp_paged_attention -- softmax attention of new tokens (a chunk, or single tokens) over the
+ * paged cache, which already holds them (vp_rope_append).
+ *   kv_len   [B] int32: tokens in the cache, the new ones included
+ *   kv       HOST pointer
+ * The other arguments are those of vp_prompt_attention.
+ */
+vp_status vp_paged_attention(const vp_attn_dims* dims, int32_t T, int32_t B, const void* q,
+                             int64_t q_stride, const int32_t* cu, const int32_t* kv_len,
+                             const vp_paged_kv* kv, void* out, int64_t out_stride, float* lse,
+                             void* ws, size_t ws_bytes, void* stream);
+
 /* Kernel classes reported by the launch profiler. */
 #define VP_KERNEL_GEMM 0
 #define VP_KERNEL_ROUTER_POOL 1
@@ -363,7 +472,9 @@ vp_status vp_router_noalloc_error(uint32_t* host_bits, void* stream);
                                    weight fold */
 #define VP_KERNEL_MERGE 9       /* token merging (vp_merge_options) and the unmerge */
 #define VP_KERNEL_HOST_COPY 10  /* host <-> device copies of vp_global_stack_host */
-#define VP_KERNEL_CLASSES 11
+#define VP_KERNEL_ROPE_APPEND 11 /* vp_rope_append */
+#define VP_KERNEL_SEQ_ATTN 12    /* vp_prompt_attention, vp_paged_attention (all their kernels) */
+#define VP_KERNEL_CLASSES 13
 
 /*
  * Launch profiler (for benchmarks; not part of the method).  Between vp_profile_begin and

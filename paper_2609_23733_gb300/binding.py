@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import math
 from ctypes import POINTER, Structure, c_char_p, c_float, c_int32, c_int64, c_size_t, c_uint32, c_void_p
 
 import numpy as np
@@ -19,10 +20,10 @@ from .build import LIB
 VP_MODE_MEAN, VP_MODE_SURROGATE, VP_MODE_FULL = 0, 1, 2
 VP_WS_ROUTER, VP_WS_LAYER, VP_WS_STACK, VP_WS_STACK_MERGE = 0, 1, 2, 3
 VP_ACT_NONE, VP_ACT_GELU = 0, 1
-VP_DEVERR_WAIT_TIMEOUT, VP_DEVERR_NAN_SALIENCY = 1, 2
+VP_DEVERR_WAIT_TIMEOUT, VP_DEVERR_NAN_SALIENCY, VP_DEVERR_PAGE = 1, 2, 4
 VP_VARIANT_MEAN_QPOOL, VP_VARIANT_MEAN_CONTEXT, VP_VARIANT_NO_RESIDUAL, VP_VARIANT_LINEAR_ATTENTION = 1, 2, 4, 8
 KERNEL_CLASSES = ["gemm", "router_pool", "router_keys", "router_r", "bin_heads", "attn_full",
-                  "surrogate", "mean", "layer_norm", "merge", "host_copy"]
+                  "surrogate", "mean", "layer_norm", "merge", "host_copy", "rope_append", "seq_attn"]
 
 STATUS = {0: "VP_OK", 1: "VP_ERR_INVALID_ARG", 2: "VP_ERR_UNSUPPORTED_SHAPE", 3: "VP_ERR_ALIGNMENT",
           4: "VP_ERR_CUDA", 5: "VP_ERR_DEVICE_TIMEOUT", 6: "VP_ERR_WORKSPACE",
@@ -66,6 +67,22 @@ class VpLayerWeights(Structure):
                 ("qk", POINTER(VpQkOptions)), ("merge", POINTER(VpMergeOptions))]
 
 
+VP_DTYPES = {torch.bfloat16: 0, torch.float16: 1}
+
+
+class VpAttnDims(Structure):
+    _fields_ = [(n, c_int32) for n in ("Hq", "Hkv", "d", "dtype", "block")] + [("scale", c_float)]
+
+
+class VpPagedKv(Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("page_table", c_void_p), ("n_pages", c_int32),
+                ("page_size", c_int32), ("table_width", c_int32)]
+
+
+class VpRopeOptions(Structure):
+    _fields_ = [("turns", c_void_p), ("rot_dim", c_int32), ("interleaved", c_int32), ("scale", c_float)]
+
+
 _lib = None
 
 # (name, restype, argtypes)
@@ -99,6 +116,16 @@ _SIGS = [
     ("vp_global_stack_host", c_int32, [POINTER(VpDims), c_int32, c_void_p, c_void_p, c_void_p,
                                        POINTER(VpLayerWeights), c_void_p, c_void_p, c_void_p, c_void_p,
                                        c_float, c_void_p, c_size_t, c_void_p]),
+    ("vp_attn_workspace_size", c_int32, [POINTER(VpAttnDims), c_int32, c_int32, POINTER(c_size_t)]),
+    ("vp_rope_append", c_int32, [POINTER(VpAttnDims), POINTER(VpRopeOptions), c_int32, c_int32, c_void_p, c_int64,
+                                 c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_void_p,
+                                 POINTER(VpPagedKv), c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_size_t,
+                                 c_void_p]),
+    ("vp_prompt_attention", c_int32, [POINTER(VpAttnDims), c_int32, c_int32, c_void_p, c_int64, c_void_p, c_int64,
+                                      c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_size_t,
+                                      c_void_p]),
+    ("vp_paged_attention", c_int32, [POINTER(VpAttnDims), c_int32, c_int32, c_void_p, c_int64, c_void_p, c_void_p,
+                                     POINTER(VpPagedKv), c_void_p, c_int64, c_void_p, c_void_p, c_size_t, c_void_p]),
     ("vp_profile_begin", c_int32, [c_int32]),
     ("vp_profile_end", c_int32, [POINTER(c_int32), POINTER(c_int32), POINTER(c_float)]),
     ("vp_global_stack", c_int32, [POINTER(VpDims), c_int32, c_void_p, POINTER(VpLayerWeights),
@@ -215,6 +242,67 @@ def layer_weights(w: dict, qk: VpQkOptions = None, merge: VpMergeOptions = None)
         lw.merge = ctypes.pointer(merge)
         lw._merge_keep = merge
     return lw
+
+
+def attn_dims(Hq, Hkv=None, d=64, dtype=torch.bfloat16, block=1, scale=None) -> VpAttnDims:
+    """vp_attn_dims of the streaming operators; scale None: 1 / sqrt(d)."""
+    if dtype not in VP_DTYPES:
+        raise ValueError("dtype must be torch.bfloat16 or torch.float16")
+    return VpAttnDims(int(Hq), int(Hq if Hkv is None else Hkv), int(d), VP_DTYPES[dtype], int(block),
+                      1.0 / math.sqrt(d) if scale is None else float(scale))
+
+
+def paged_kv(k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor) -> VpPagedKv:
+    """vp_paged_kv of a cache: k, v [n_pages][Hkv][page_size][d], page_table [B][width] int32."""
+    if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or k.dtype not in VP_DTYPES:
+        raise ValueError("k and v: one 16-bit type and one shape [n_pages][Hkv][page_size][d]")
+    if page_table.dim() != 2 or page_table.dtype != torch.int32:
+        raise ValueError("page_table: int32 [sequences][pages of a sequence]")
+    o = VpPagedKv(_p(k), _p(v), _p(page_table), k.shape[0], k.shape[2], page_table.shape[1])
+    o._keep = (k, v, page_table)
+    o._heads = (k.shape[1], k.shape[3], VP_DTYPES[k.dtype])
+    o._rows = page_table.shape[0]
+    return o
+
+
+def rope_turns(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+               original_len: int = 0, low: float = 1.0, high: float = 32.0) -> torch.Tensor:
+    """The table of vp_rope_options: turns per position of each of the rot_dim / 2 pairs, as 64-bit
+    fractions of a turn (int64, on the CPU).  Pair i turns by base^(-2 i / rot_dim) radians per
+    position.  For contexts longer than the original_len positions of the training, by ``factor``:
+      "linear"  every frequency divided by factor (positions interpolated)
+      "base"    the base raised by factor^(rot_dim / (rot_dim - 2)): the slowest pair is divided by
+                factor, the fastest kept
+      "parts"   by the turns a pair makes within original_len: divided by factor below ``low`` turns,
+                kept above ``high``, mixed linearly in between
+    """
+    if rot_dim < 0 or rot_dim % 2 or not base > 1 or not factor >= 1:
+        raise ValueError("rot_dim must be even, base > 1 and factor >= 1")
+    if scaling not in ("none", "linear", "base", "parts"):
+        raise ValueError(f"unknown scaling {scaling!r}")
+    if scaling == "parts" and (original_len < 1 or not high > low):
+        raise ValueError("scaling 'parts' needs original_len >= 1 and high > low")
+    if scaling == "base" and rot_dim > 2:
+        base = base * factor ** (rot_dim / (rot_dim - 2))
+    turns = []
+    for i in range(rot_dim // 2):
+        f = base ** (-2.0 * i / rot_dim) / (2 * math.pi)
+        if scaling == "linear":
+            f /= factor
+        elif scaling == "parts":
+            keep = min(1.0, max(0.0, (original_len * f - low) / (high - low)))
+            f = f * (keep + (1 - keep) / factor)
+        turns.append(int(f * 2.0 ** 64))
+    return torch.tensor(turns, dtype=torch.int64)
+
+
+def rope_options(turns: torch.Tensor, interleaved: bool = False, scale: float = 1.0) -> VpRopeOptions:
+    """vp_rope_options from the device table of ``rope_turns`` (int64 [rot_dim / 2])."""
+    if turns.dtype != torch.int64 or turns.dim() != 1:
+        raise ValueError("turns: int64 [rot_dim / 2]")
+    o = VpRopeOptions(_p(turns) if turns.numel() else None, 2 * turns.numel(), 1 if interleaved else 0, float(scale))
+    o._keep = turns
+    return o
 
 
 def to_device(w: dict, device="cuda") -> dict:
@@ -347,6 +435,96 @@ def vp_global_stack_host(dm, x_in, x_out, x_dev, layers, force_modes, modes_out,
     _check(lib().vp_global_stack_host(ctypes.byref(dm), len(layers), _host_p(x_in), _host_p(x_out), _p(x_dev), arr,
                                       _p(force_modes), _p(modes_out), _p(s_out), _p(s_attn_out), float(ln_eps),
                                       _p(ws), ws.numel(), _stream(stream)), "vp_global_stack_host")
+
+
+def vp_attn_workspace_size(dims: VpAttnDims, T: int, B: int) -> int:
+    n = c_size_t(0)
+    _check(lib().vp_attn_workspace_size(ctypes.byref(dims), int(T), int(B), ctypes.byref(n)),
+           "vp_attn_workspace_size")
+    return n.value
+
+
+def attn_workspace(dims: VpAttnDims, T: int, B: int, device="cuda") -> torch.Tensor:
+    """A device workspace for up to T packed tokens in up to B sequences, its error word zero."""
+    ws = torch.empty(vp_attn_workspace_size(dims, T, B), dtype=torch.uint8, device=device)
+    ws[:256].zero_()
+    return ws
+
+
+def _rows_p(t, heads, dims, T=None):
+    """(address, token stride) of a [T][heads][d] tensor whose heads and channels are contiguous."""
+    if t is None:
+        return None, 0
+    sh, st = t.shape, t.stride()
+    if len(sh) != 3 or sh[1] != heads or sh[2] != dims.d or (T is not None and sh[0] != T):
+        raise ValueError(f"expected [{'T' if T is None else T}][{heads}][{dims.d}], got {list(sh)}")
+    if st[2] != 1 or (st[1] != dims.d and heads > 1):
+        raise ValueError("heads and channels must be contiguous")
+    if VP_DTYPES.get(t.dtype, -1) != dims.dtype:
+        raise ValueError(f"the tensor's type {t.dtype} is not that of dims")
+    if not t.is_cuda:
+        raise ValueError("device tensors are required (the library has no CPU path)")
+    # a single token has no stride of its own: any legal one stands for it
+    return t.data_ptr(), st[0] if sh[0] > 1 else heads * dims.d
+
+
+def _ints_p(t, n, what):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.numel() != n:
+        raise ValueError(f"{what}: int32 with {n} values")
+    return _p(t)
+
+
+def _kv_ref(kv, dims, B):
+    if kv is None:
+        return None
+    if kv._heads != (dims.Hkv, dims.d, dims.dtype):
+        raise ValueError("the cache's heads, head dim or type are not those of dims")
+    if kv._rows < B:
+        raise ValueError(f"the page table has {kv._rows} rows for {B} sequences")
+    return ctypes.byref(kv)
+
+
+def vp_rope_append(dims: VpAttnDims, rope: VpRopeOptions, q, k, v, cu, kv_len, positions, kv: VpPagedKv = None,
+                   q_out=None, k_out=None, ws=None, stream=None):
+    """Rotates q into q_out and k into the cache (and / or k_out), and writes v to the cache."""
+    T, B = k.shape[0], cu.numel() - 1
+    qp, qs = _rows_p(q, dims.Hq, dims, T)
+    kp, ks = _rows_p(k, dims.Hkv, dims, T)
+    vp, vs = _rows_p(v, dims.Hkv, dims, T)
+    qo, qos = _rows_p(q_out, dims.Hq, dims, T)
+    ko, kos = _rows_p(k_out, dims.Hkv, dims, T)
+    _check(lib().vp_rope_append(ctypes.byref(dims), ctypes.byref(rope), T, B, qp, qs, kp, ks, vp, vs,
+                                _ints_p(cu, B + 1, "cu"), _ints_p(kv_len, B, "kv_len"),
+                                _ints_p(positions, T, "positions"), _kv_ref(kv, dims, B), qo, qos, ko, kos, _p(ws),
+                                0 if ws is None else ws.numel(), _stream(stream)), "vp_rope_append")
+
+
+def _lse_p(lse, T, dims):
+    if lse is not None and (lse.dtype != torch.float32 or lse.numel() != T * dims.Hq):
+        raise ValueError(f"lse: float32 [{T}][{dims.Hq}]")
+    return _p(lse)
+
+
+def vp_prompt_attention(dims: VpAttnDims, q, k, v, cu, out, lse, ws, stream=None):
+    T, B = q.shape[0], cu.numel() - 1
+    qp, qs = _rows_p(q, dims.Hq, dims)
+    kp, ks = _rows_p(k, dims.Hkv, dims, T)
+    vp, vs = _rows_p(v, dims.Hkv, dims, T)
+    op, os_ = _rows_p(out, dims.Hq, dims, T)
+    _check(lib().vp_prompt_attention(ctypes.byref(dims), T, B, qp, qs, kp, ks, vp, vs, _ints_p(cu, B + 1, "cu"), op,
+                                     os_, _lse_p(lse, T, dims), _p(ws), ws.numel(), _stream(stream)),
+           "vp_prompt_attention")
+
+
+def vp_paged_attention(dims: VpAttnDims, q, cu, kv_len, kv: VpPagedKv, out, lse, ws, stream=None):
+    T, B = q.shape[0], cu.numel() - 1
+    qp, qs = _rows_p(q, dims.Hq, dims)
+    op, os_ = _rows_p(out, dims.Hq, dims, T)
+    _check(lib().vp_paged_attention(ctypes.byref(dims), T, B, qp, qs, _ints_p(cu, B + 1, "cu"),
+                                    _ints_p(kv_len, B, "kv_len"), _kv_ref(kv, dims, B), op, os_,
+                                    _lse_p(lse, T, dims), _p(ws), ws.numel(), _stream(stream)), "vp_paged_attention")
 
 
 def vp_profile_begin(max_launches: int):

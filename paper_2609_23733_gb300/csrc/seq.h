@@ -1,0 +1,136 @@
+// Streaming operators (rotary append, prompt attention, attention over the paged cache):
+// launch arguments and device helpers shared by their kernels (not part of the ABI).
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "internal.h"
+
+namespace vp {
+
+// The paged cache (vp_paged_kv) as the kernels see it.
+struct PagedKv {
+  uint16_t* k;
+  uint16_t* v;
+  const int32_t* table;
+  int32_t n_pages, page_size, log2_page, width;
+};
+
+struct RopeAppendArgs {
+  int T, B, Hq, Hkv, d, fp16;
+  int rot, interleaved;
+  float scale;
+  const int64_t* turns;
+  const uint16_t* q;
+  const uint16_t* k;
+  const uint16_t* v;
+  int64_t q_stride, k_stride, v_stride;
+  const int32_t* cu;
+  const int32_t* kv_len;     // NULL: no cache
+  const int32_t* positions;  // NULL: the slot
+  PagedKv kv;                // kv.k NULL: no cache
+  uint16_t* q_out;
+  uint16_t* k_out;
+  int64_t q_out_stride, k_out_stride;
+  unsigned int* err;         // NULL: not recorded
+};
+cudaError_t launch_rope_append(const RopeAppendArgs& a, int num_sms, cudaStream_t st);
+
+struct SeqAttnArgs {
+  int T, B, Hq, Hkv, group, d, fp16;
+  int block;
+  float scale_log2;          // scale x log2(e)
+  const uint16_t* q;
+  int64_t q_stride;
+  const uint16_t* k;         // prompts: packed keys and values; paged: NULL (in kv)
+  const uint16_t* v;
+  int64_t k_stride, v_stride;
+  const int32_t* cu;
+  const int32_t* kv_len;     // paged only
+  PagedKv kv;                // kv.k NULL: prompts
+  uint16_t* out;
+  int64_t out_stride;
+  float* lse;                // [T][Hq] or NULL
+  unsigned int* err;
+};
+cudaError_t launch_seq_attention(const SeqAttnArgs& a, int num_sms, cudaStream_t st);
+
+#ifdef __CUDACC__
+
+// One sequence: its new tokens [q0, q0 + ql) among the T packed ones, and the keys [0, kl).
+struct Seq {
+  int q0, ql, kl;
+};
+
+// Sequence b, clamped so that nothing outside the T tokens or the page table is touched.
+__device__ __forceinline__ Seq load_seq(const SeqAttnArgs& a, int b) {
+  Seq s;
+  const int c0 = a.cu[b], c1 = a.cu[b + 1];
+  s.q0 = min(max(c0, 0), a.T);
+  s.ql = min(max(c1, s.q0), a.T) - s.q0;
+  if (a.kv.k) {
+    const long long cap = (long long)a.kv.width << a.kv.log2_page;
+    const int n = a.kv_len[b];
+    s.kl = (int)min((long long)max(n, 0), cap);
+    if (s.kl != n && a.err) atomicOr(a.err, VP_DEVERR_PAGE);
+  } else {
+    s.kl = s.ql;
+  }
+  return s;
+}
+
+// Keys [0, lim) are visible to new token i (0 <= i < ql).  lim <= 0: none.
+__device__ __forceinline__ int row_limit(int i, int ql, int kl, int block) {
+  if (block == 0) return kl;
+  const int rest = ql - i, step = block - i % block;  // both at least 1
+  return kl - ql + i + min(rest, step);
+}
+
+// The last sequence b < B with cu[b] <= t (0 if there is none): the owner of token t where cu
+// is ascending; always a valid index.
+__device__ __forceinline__ int seq_of_token(const int32_t* cu, int B, int t) {
+  int lo = 0, hi = B - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (cu[mid] <= t)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  return lo;
+}
+
+// 16-bit storage types.
+template <bool F16>
+__device__ __forceinline__ float to_float(uint16_t u) {
+  if constexpr (F16)
+    return __half2float(__ushort_as_half(u));
+  else
+    return __uint_as_float((uint32_t)u << 16);
+}
+template <bool F16>
+__device__ __forceinline__ float2 unpack2(uint32_t u) {
+  if constexpr (F16) {
+    __half2 h = *reinterpret_cast<__half2*>(&u);
+    return __half22float2(h);
+  } else {
+    return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
+  }
+}
+template <bool F16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  if constexpr (F16) {
+    __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<uint32_t*>(&h);
+  } else {
+    __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t*>(&h);
+  }
+}
+
+#endif  // __CUDACC__
+
+}  // namespace vp
