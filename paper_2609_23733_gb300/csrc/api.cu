@@ -10,6 +10,7 @@
 #include <mutex>
 
 #include "internal.h"
+#include "seq.h"
 #include "vp.h"
 
 namespace vp {
@@ -93,9 +94,8 @@ void prof_after(cudaStream_t st) {
 int device_sm_count() { return dev_info().sms; }
 bool device_is_sm103() { return dev_info().sm103 == 1; }
 
-cudaError_t make_tmap_bf16_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows,
-                              uint64_t pitch_elems, uint32_t box_cols, uint32_t box_rows,
-                              int swizzle_bytes) {
+namespace {
+bool load_encode_fn() {
   std::call_once(g_encode_once, [] {
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult q;
@@ -104,7 +104,34 @@ cudaError_t make_tmap_bf16_2d(CUtensorMap* map, const void* base, uint64_t cols,
         q == cudaDriverEntryPointSuccess)
       g_encode = reinterpret_cast<EncodeTiledFn>(fn);
   });
-  if (!g_encode) return cudaErrorNotSupported;
+  return g_encode != nullptr;
+}
+}  // namespace
+
+cudaError_t make_tmap_16bit_4d(CUtensorMap* map, const void* base, bool fp16,
+                               const uint64_t dims[4], const uint64_t strides[3],
+                               const uint32_t box[4]) {
+  if (!load_encode_fn()) return cudaErrorNotSupported;
+  cuuint64_t d[4], s[3];
+  cuuint32_t b[4];
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  for (int i = 0; i < 4; ++i) {
+    d[i] = dims[i];
+    b[i] = box[i];
+  }
+  for (int i = 0; i < 3; ++i) s[i] = strides[i] * 2;
+  const CUresult r = g_encode(map,
+                              fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                              4, const_cast<void*>(base), d, s, b, estr,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+cudaError_t make_tmap_bf16_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows,
+                              uint64_t pitch_elems, uint32_t box_cols, uint32_t box_rows,
+                              int swizzle_bytes) {
+  if (!load_encode_fn()) return cudaErrorNotSupported;
   const cuuint64_t dims[2] = {cols, rows};
   const cuuint64_t strides[1] = {pitch_elems * 2};
   const cuuint32_t box[2] = {box_cols, box_rows};

@@ -56,9 +56,36 @@ struct SeqAttnArgs {
   float* lse;                // [T][Hq] or NULL
   unsigned int* err;
 };
-cudaError_t launch_seq_attention(const SeqAttnArgs& a, int num_sms, cudaStream_t st);
+
+// Attention's scratch inside the caller's workspace, after the error word.
+struct SeqScratch {
+  int* head;        // [16] counts written by the plan (kPlan*)
+  int4* items;      // [cap_items][2] work items
+  int4* splits;     // [cap_splits][2] tiles cut into several pieces
+  int* tile_off;    // [B + 1] query tiles before sequence b
+  float* part_o;    // partial outputs of pieces: [slot][rows][d]
+  float2* part_ml;  // [slot][rows] (m, l)
+};
+constexpr int kMaxCtas = 160;               // CTAs of the tile kernel, at most (one per SM)
+constexpr int kMaxSlots = 4 * kMaxCtas;     // pieces of cut tiles, at most (all kv heads)
+// Query rows of one work item of the tile kernel: the chains of 128 rows that share its keys.
+__host__ __device__ constexpr int seq_chains(int d) { return d == 64 ? 3 : 2; }
+size_t seq_scratch_bytes(int d, int Hq, int Hkv, int64_t T, int64_t B);
+SeqScratch carve_seq_scratch(void* ws, int d, int Hq, int Hkv, int64_t T, int64_t B);
+
+cudaError_t launch_seq_attention(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms,
+                                 cudaStream_t st);
+
+// 4-D tensor map of 16-bit values with a 64-element (128-byte) inner box, 128-byte swizzle, zero
+// fill out of bounds; strides in elements (dims 1..3).
+cudaError_t make_tmap_16bit_4d(CUtensorMap* map, const void* base, bool fp16,
+                               const uint64_t dims[4], const uint64_t strides[3],
+                               const uint32_t box[4]);
 
 #ifdef __CUDACC__
+}  // namespace vp
+#include "common.cuh"
+namespace vp {
 
 // One sequence: its new tokens [q0, q0 + ql) among the T packed ones, and the keys [0, kl).
 struct Seq {
@@ -129,6 +156,39 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<uint32_t*>(&h);
   }
+}
+
+__device__ __forceinline__ void tma_load_4d(void* smem_dst, const void* tmap, uint64_t* bar, int x,
+                                            int y, int z, int w) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(smem_u32(smem_dst)),
+      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
+      : "memory");
+}
+
+__device__ __forceinline__ void pdl_launch_dependents() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// Whether a pair of 16-bit values holds an infinity or a NaN (all exponent bits set): adding one
+// to the exponent field carries into the sign place exactly then.
+template <bool F16>
+__device__ __forceinline__ bool nonfinite2(uint32_t u) {
+  if constexpr (F16)
+    return (((u & 0x7C007C00u) + 0x04000400u) & 0x80008000u) != 0;
+  else
+    return (((u & 0x7F807F80u) + 0x00800080u) & 0x80008000u) != 0;
+}
+// The pair with its infinities and NaNs replaced by 0.
+template <bool F16>
+__device__ __forceinline__ uint32_t finite2(uint32_t u) {
+  const uint32_t t = F16 ? (((u & 0x7C007C00u) + 0x04000400u) & 0x80008000u)
+                         : (((u & 0x7F807F80u) + 0x00800080u) & 0x80008000u);
+  if (t & 0x8000u) u &= 0xFFFF0000u;
+  if (t & 0x80000000u) u &= 0x0000FFFFu;
+  return u;
 }
 
 #endif  // __CUDACC__

@@ -92,7 +92,13 @@ SeqAttnArgs make_args(const vp_attn_dims* dm, int32_t T, int32_t B, const void* 
   return a;
 }
 
-size_t attn_ws_bytes(const vp_attn_dims*, int32_t, int32_t) { return 256; }
+size_t attn_ws_bytes(const vp_attn_dims* dm, int32_t T, int32_t B) {
+  return seq_scratch_bytes(dm->d, dm->Hq, dm->Hkv, T, B);
+}
+
+SeqScratch carve(const vp_attn_dims* dm, int32_t T, int32_t B, void* ws) {
+  return carve_seq_scratch(ws, dm->d, dm->Hq, dm->Hkv, T, B);
+}
 
 }  // namespace
 
@@ -185,7 +191,7 @@ vp_status vp_prompt_attention(const vp_attn_dims* dims, int32_t T, int32_t B, co
   a.v = static_cast<const uint16_t*>(v);
   a.k_stride = k_stride;
   a.v_stride = v_stride;
-  return from_cuda(launch_seq_attention(a, device_sm_count(), static_cast<cudaStream_t>(stream)));
+  return from_cuda(launch_seq_attention(a, carve(dims, T, B, ws), device_sm_count(), static_cast<cudaStream_t>(stream)));
 }
 
 vp_status vp_paged_attention(const vp_attn_dims* dims, int32_t T, int32_t B, const void* q,
@@ -205,7 +211,7 @@ vp_status vp_paged_attention(const vp_attn_dims* dims, int32_t T, int32_t B, con
   SeqAttnArgs a = make_args(dims, T, B, q, q_stride, cu, out, out_stride, lse, ws);
   a.kv_len = kv_len;
   a.kv = make_kv(kv);
-  return from_cuda(launch_seq_attention(a, device_sm_count(), static_cast<cudaStream_t>(stream)));
+  return from_cuda(launch_seq_attention(a, carve(dims, T, B, ws), device_sm_count(), static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"
