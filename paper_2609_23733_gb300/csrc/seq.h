@@ -73,6 +73,17 @@ __host__ __device__ constexpr int seq_chains(int d) { return d == 64 ? 3 : 2; }
 size_t seq_scratch_bytes(int d, int Hq, int Hkv, int64_t T, int64_t B);
 SeqScratch carve_seq_scratch(void* ws, int d, int Hq, int Hkv, int64_t T, int64_t B);
 
+// Few rows per sequence (seq_rows.cu): items of kSmallRows rows.
+constexpr int kSmallRows = 16;
+__host__ __device__ constexpr int small_rows_ctas_per_sm(int d) { return d == 64 ? 3 : 2; }
+static_assert(2 * 3 * kMaxCtas * kSmallRows <= kMaxSlots * 2 * 128, "its parts fit the scratch");
+cudaError_t launch_seq_rows(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms, cudaStream_t st);
+
+// Tensor maps of the keys and values, boxes of 64 channels x min(page, tile_keys) keys.
+cudaError_t make_kv_maps(const SeqAttnArgs& a, int tile_keys, CUtensorMap* mk, CUtensorMap* mv);
+// A launch whose kernel may start before the one ahead of it in the stream has ended.
+cudaError_t launch_pdl(const void* fn, int grid, int threads, int smem, cudaStream_t st, void** args);
+
 cudaError_t launch_seq_attention(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms,
                                  cudaStream_t st);
 

@@ -763,20 +763,6 @@ ScratchLayout scratch_layout(int d, int Hq, int Hkv, int64_t T, int64_t B) {
   return l;
 }
 
-cudaError_t launch_pdl(const void* fn, int grid, int threads, int smem, cudaStream_t st, void** args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelExC(&cfg, fn, args);
-}
-
 template <int D, bool F16, bool kPaged>
 cudaError_t launch_tiles(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms, cudaStream_t st) {
   using C = Cfg<D>;
@@ -788,20 +774,7 @@ cudaError_t launch_tiles(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms
   const uint32_t qb[4] = {64, (uint32_t)g, 1, (uint32_t)tpt};
   cudaError_t e = make_tmap_16bit_4d(&mq, a.q, F16, qd, qs, qb);
   if (e != cudaSuccess) return e;
-  if (kPaged) {
-    const uint64_t ps = a.kv.page_size;
-    const uint64_t kd[4] = {D, ps, H, (uint64_t)a.kv.n_pages};
-    const uint64_t ks[3] = {D, ps * D, H * ps * D};
-    const uint32_t kb[4] = {64, (uint32_t)(ps < kBN ? ps : kBN), 1, 1};
-    e = make_tmap_16bit_4d(&mk, a.kv.k, F16, kd, ks, kb);
-    if (e == cudaSuccess) e = make_tmap_16bit_4d(&mv, a.kv.v, F16, kd, ks, kb);
-  } else {
-    const uint64_t kd[4] = {D, (uint64_t)a.T, H, 1};
-    const uint64_t ks[3] = {(uint64_t)a.k_stride, D, H * D}, vs[3] = {(uint64_t)a.v_stride, D, H * D};
-    const uint32_t kb[4] = {64, kBN, 1, 1};
-    e = make_tmap_16bit_4d(&mk, a.k, F16, kd, ks, kb);
-    if (e == cudaSuccess) e = make_tmap_16bit_4d(&mv, a.v, F16, kd, vs, kb);
-  }
+  e = make_kv_maps(a, kBN, &mk, &mv);
   if (e != cudaSuccess) return e;
   const int P = num_sms < kMaxCtas ? num_sms : kMaxCtas;
   constexpr int smem = (int)sizeof(TileSmem<D>) + 1024;
@@ -825,6 +798,38 @@ cudaError_t launch_tiles(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms
 }
 
 }  // namespace
+
+cudaError_t launch_pdl(const void* fn, int grid, int threads, int smem, cudaStream_t st, void** args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelExC(&cfg, fn, args);
+}
+
+cudaError_t make_kv_maps(const SeqAttnArgs& a, int tile_keys, CUtensorMap* mk, CUtensorMap* mv) {
+  const uint64_t d = a.d, H = a.Hkv;
+  if (a.kv.k) {
+    const uint64_t ps = a.kv.page_size;
+    const uint64_t dims[4] = {d, ps, H, (uint64_t)a.kv.n_pages};
+    const uint64_t strides[3] = {d, ps * d, H * ps * d};
+    const uint32_t box[4] = {64, ps < (uint64_t)tile_keys ? (uint32_t)ps : (uint32_t)tile_keys, 1, 1};
+    const cudaError_t e = make_tmap_16bit_4d(mk, a.kv.k, a.fp16 != 0, dims, strides, box);
+    return e != cudaSuccess ? e : make_tmap_16bit_4d(mv, a.kv.v, a.fp16 != 0, dims, strides, box);
+  }
+  // Packed keys: one page of T rows.
+  const uint64_t dims[4] = {d, (uint64_t)a.T, H, 1};
+  const uint64_t ks[3] = {(uint64_t)a.k_stride, d, H * d}, vs[3] = {(uint64_t)a.v_stride, d, H * d};
+  const uint32_t box[4] = {64, (uint32_t)tile_keys, 1, 1};
+  const cudaError_t e = make_tmap_16bit_4d(mk, a.k, a.fp16 != 0, dims, ks, box);
+  return e != cudaSuccess ? e : make_tmap_16bit_4d(mv, a.v, a.fp16 != 0, dims, vs, box);
+}
 
 size_t seq_scratch_bytes(int d, int Hq, int Hkv, int64_t T, int64_t B) {
   return scratch_layout(d, Hq, Hkv, T, B).end;
@@ -852,7 +857,12 @@ cudaError_t launch_seq_attention(const SeqAttnArgs& a, const SeqScratch& sc, int
       {{launch_tiles<128, false, false>, launch_tiles<128, false, true>},
        {launch_tiles<128, true, false>, launch_tiles<128, true, true>}}};
   prof_before(VP_KERNEL_SEQ_ATTN, st);
-  const cudaError_t e = table[a.d == 128][a.fp16 != 0][a.kv.k != nullptr](a, sc, num_sms, st);
+  // Up to 16 rows per sequence on average: the keys are read once by either kernel, and the one for
+  // few rows has more of them in flight and no TMEM round trip; above, it would read them again
+  // for every 16 rows.
+  const bool few = (long long)a.T * a.group <= (long long)kSmallRows * a.B;
+  const cudaError_t e = few ? launch_seq_rows(a, sc, num_sms, st)
+                            : table[a.d == 128][a.fp16 != 0][a.kv.k != nullptr](a, sc, num_sms, st);
   prof_after(st);
   return e;
 }
