@@ -18,7 +18,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(BUILD, "libvp.so")
 SOURCES = ["api.cu", "router.cu", "attn_full.cu", "heads_cheap.cu", "heads_cheap_tc.cu", "gemm.cu",
            "layernorm.cu", "router_noalloc.cu", "merge.cu", "host_copy.cu", "linear_attn_tc.cu",
-           "rope_append.cu", "seq_attn.cu", "seq_rows.cu", "seq_api.cu"]
+           "rope_append.cu", "seq_attn.cu", "seq_rows.cu", "seq_join.cu", "seq_api.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -59,30 +59,34 @@ struct SeqAttnArgs {
 
 // Attention's scratch inside the caller's workspace, after the error word.
 struct SeqScratch {
-  int* head;        // [16] counts written by the plan (kPlan*)
-  int4* items;      // [cap_items][2] work items
-  int4* splits;     // [cap_splits][2] tiles cut into several pieces
-  int* tile_off;    // [B + 1] query tiles before sequence b
-  float* part_o;    // partial outputs of pieces: [slot][rows][d]
+  int4* recs;       // [CTAs][2] items cut between CTAs: {parts (0: none), kv head, first token or
+                    // row tile, sequence}, {q0, ql, kl, first part's slot}; part i > 0 lies in slot
+                    // 2 (cta + i)
+  float* part_o;    // partial outputs, unnormalised: [slot][rows][d]
   float2* part_ml;  // [slot][rows] (m, l)
 };
-constexpr int kMaxCtas = 160;               // CTAs of the tile kernel, at most (one per SM)
-constexpr int kMaxSlots = 4 * kMaxCtas;     // pieces of cut tiles, at most (all kv heads)
-// Query rows of one work item of the tile kernel: the chains of 128 rows that share its keys.
+constexpr int kMaxCtas = 160;            // CTAs of the tile kernel, at most (one per SM)
+constexpr int kMaxSlots = 2 * kMaxCtas;  // a CTA's run has at most two items in part
+// Chains of 128 query rows of an item of the tile kernel.
 __host__ __device__ constexpr int seq_chains(int d) { return d == 64 ? 3 : 2; }
-size_t seq_scratch_bytes(int d, int Hq, int Hkv, int64_t T, int64_t B);
-SeqScratch carve_seq_scratch(void* ws, int d, int Hq, int Hkv, int64_t T, int64_t B);
+size_t seq_scratch_bytes(int d);
+SeqScratch carve_seq_scratch(void* ws, int d);
 
 // Few rows per sequence (seq_rows.cu): items of kSmallRows rows.
 constexpr int kSmallRows = 16;
 __host__ __device__ constexpr int small_rows_ctas_per_sm(int d) { return d == 64 ? 3 : 2; }
-static_assert(2 * 3 * kMaxCtas * kSmallRows <= kMaxSlots * 2 * 128, "its parts fit the scratch");
+constexpr int kMaxRecs = 3 * kMaxCtas;   // CTAs of either kernel, at most
+static_assert(2 * kMaxRecs * kSmallRows <= kMaxSlots * 2 * 128, "its parts fit the scratch");
 cudaError_t launch_seq_rows(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms, cudaStream_t st);
+
+// Joins the items cut between the `ctas` CTAs of the kernel ahead (seq_join.cu).
+cudaError_t launch_seq_join(const SeqAttnArgs& a, const SeqScratch& sc, bool tiles, int ctas,
+                            cudaStream_t st);
 
 // Tensor maps of the keys and values, boxes of 64 channels x min(page, tile_keys) keys.
 cudaError_t make_kv_maps(const SeqAttnArgs& a, int tile_keys, CUtensorMap* mk, CUtensorMap* mv);
 // A launch whose kernel may start before the one ahead of it in the stream has ended.
-cudaError_t launch_pdl(const void* fn, int grid, int threads, int smem, cudaStream_t st, void** args);
+cudaError_t launch_pdl(const void* fn, dim3 grid, int threads, int smem, cudaStream_t st, void** args);
 
 cudaError_t launch_seq_attention(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms,
                                  cudaStream_t st);

@@ -92,14 +92,6 @@ SeqAttnArgs make_args(const vp_attn_dims* dm, int32_t T, int32_t B, const void* 
   return a;
 }
 
-size_t attn_ws_bytes(const vp_attn_dims* dm, int32_t T, int32_t B) {
-  return seq_scratch_bytes(dm->d, dm->Hq, dm->Hkv, T, B);
-}
-
-SeqScratch carve(const vp_attn_dims* dm, int32_t T, int32_t B, void* ws) {
-  return carve_seq_scratch(ws, dm->d, dm->Hq, dm->Hkv, T, B);
-}
-
 }  // namespace
 
 extern "C" {
@@ -108,7 +100,7 @@ vp_status vp_attn_workspace_size(const vp_attn_dims* dims, int32_t T, int32_t B,
   VP_TRY(check_attn_dims(dims));
   VP_TRY(check_counts(T, B));
   if (!bytes) return VP_ERR_INVALID_ARG;
-  *bytes = attn_ws_bytes(dims, T, B);
+  *bytes = seq_scratch_bytes(dims->d);
   return VP_OK;
 }
 
@@ -182,7 +174,7 @@ vp_status vp_prompt_attention(const vp_attn_dims* dims, int32_t T, int32_t B, co
   VP_TRY(check_rows(k, k_stride, dims->Hkv, dims->d));
   VP_TRY(check_rows(v, v_stride, dims->Hkv, dims->d));
   VP_TRY(check_rows(out, out_stride, dims->Hq, dims->d));
-  if (!ws || ws_bytes < attn_ws_bytes(dims, T, B)) return VP_ERR_WORKSPACE;
+  if (!ws || ws_bytes < seq_scratch_bytes(dims->d)) return VP_ERR_WORKSPACE;
   if (!aligned16(ws)) return VP_ERR_ALIGNMENT;
   if (T == 0) return VP_OK;
   if (!device_is_sm103()) return VP_ERR_UNSUPPORTED_DEVICE;
@@ -191,7 +183,7 @@ vp_status vp_prompt_attention(const vp_attn_dims* dims, int32_t T, int32_t B, co
   a.v = static_cast<const uint16_t*>(v);
   a.k_stride = k_stride;
   a.v_stride = v_stride;
-  return from_cuda(launch_seq_attention(a, carve(dims, T, B, ws), device_sm_count(), static_cast<cudaStream_t>(stream)));
+  return from_cuda(launch_seq_attention(a, carve_seq_scratch(ws, dims->d), device_sm_count(), static_cast<cudaStream_t>(stream)));
 }
 
 vp_status vp_paged_attention(const vp_attn_dims* dims, int32_t T, int32_t B, const void* q,
@@ -204,14 +196,14 @@ vp_status vp_paged_attention(const vp_attn_dims* dims, int32_t T, int32_t B, con
   VP_TRY(check_rows(q, q_stride, dims->Hq, dims->d));
   VP_TRY(check_rows(out, out_stride, dims->Hq, dims->d));
   VP_TRY(check_kv(kv));
-  if (!ws || ws_bytes < attn_ws_bytes(dims, T, B)) return VP_ERR_WORKSPACE;
+  if (!ws || ws_bytes < seq_scratch_bytes(dims->d)) return VP_ERR_WORKSPACE;
   if (!aligned16(ws)) return VP_ERR_ALIGNMENT;
   if (T == 0) return VP_OK;
   if (!device_is_sm103()) return VP_ERR_UNSUPPORTED_DEVICE;
   SeqAttnArgs a = make_args(dims, T, B, q, q_stride, cu, out, out_stride, lse, ws);
   a.kv_len = kv_len;
   a.kv = make_kv(kv);
-  return from_cuda(launch_seq_attention(a, carve(dims, T, B, ws), device_sm_count(), static_cast<cudaStream_t>(stream)));
+  return from_cuda(launch_seq_attention(a, carve_seq_scratch(ws, dims->d), device_sm_count(), static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -2,16 +2,15 @@
 // cache (vp_paged_attention), on the sm_103a tensor cores: o = sum_j p_j v_j / sum_j p_j over the
 // keys j < lim(i) that row (token i, head h) sees, p_j = 2^(s_j - m), s_j = scale log2(e) q . k_j.
 //
-// Three kernels, chained by programmatic dependent launch:
-//   seq_plan_kernel     one CTA reads the lengths and lists the work.  A tile is kChains x (128 /
-//       group) tokens of a sequence with all heads of one kv head's group (row = token x group +
-//       head, so K and V are read once for the group).  Tiles whose keys are more than an even
-//       share (half of the total over the CTAs) are cut along the keys into pieces of
-//       at most that, and the list is ordered by length, longest first.
-//   seq_tile_kernel     persistent CTAs, one per SM, take items of the list (x kv heads) back and
-//       forth: CTA c the items c, 2 P - 1 - c, 2 P + c, ... of P CTAs, which evens out a list in
-//       descending order without a counter.
-//   seq_combine_kernel  joins the pieces of cut tiles, one warp per row, in the pieces' order.
+// Work.  A tile is kChains x (128 / group) tokens of a sequence with all heads of one kv head's group
+// (row = token x group + head, so K and V are read once for the group).  The work is the
+// sequence of units (tile, kv head, 64 keys that the tile's last row sees); CTA c of P (one per SM)
+// takes an equal run of them, whatever items (tile, kv head) they belong to, so that all CTAs end
+// together for any mix of lengths (a cut within a sixteenth of a share from an item's end moves
+// there).  Each CTA finds its run by a scan of the lengths.  An item that a CTA holds
+// in part leaves its unnormalised output; seq_join_kernel (a programmatic dependent launch)
+// joins the parts in order.  Against whole items in descending order with long ones halved (a
+// list written by a kernel ahead): see the figures at launch_tiles.
 //
 // The tile kernel.  The kChains 128-row tiles of an item run as independent chains that share the
 // K / V ring (64 keys per tile): the tensor core works for one chain while another's softmax runs.
@@ -30,6 +29,8 @@
 // tensor core needs.  Every wait is bounded; a CTA that gives up lets its copies and MMAs land.
 #include <math.h>
 
+#include <type_traits>
+
 #include "seq.h"
 
 namespace vp {
@@ -41,129 +42,101 @@ constexpr int kBN = 64;    // keys of a tile
 constexpr float kUnset = -1e30f;           // running maximum before the first visible key
 constexpr float kRescaleThreshold = 8.f;   // log2 units
 
-// Counts in SeqScratch::head.
-constexpr int kPlanItems = 0, kPlanSplits = 1;
-constexpr int kPlanThreads = 1024;
-constexpr int kBuckets = 512;
-
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
-// The sequence's keys that rows up to the last of [t0, t0 + n) see, in tiles.
-__device__ __forceinline__ int tiles_seen(int last_token, const Seq& s, int block) {
-  const int lim = row_limit(last_token, s.ql, s.kl, block);
+// Key tiles that a token sees.
+__device__ __forceinline__ int tiles_seen(int token, const Seq& s, int block) {
+  const int lim = row_limit(token, s.ql, s.kl, block);
   return lim > 0 ? ceil_div(lim, kBN) : 0;
 }
 
-// Inclusive scan over the CTA's kPlanThreads values; *total: their sum.
-__device__ __forceinline__ int block_scan(int v, int* s_warp, int* total) {
-  const int lane = lane_id(), w = warp_id();
-#pragma unroll
-  for (int k = 1; k < 32; k <<= 1) {
-    const int u = __shfl_up_sync(0xffffffffu, v, k);
-    if (lane >= k) v += u;
-  }
-  __syncthreads();
-  if (lane == 31) s_warp[w] = v;
-  __syncthreads();
-  if (w == 0) {
-    int x = s_warp[lane];
-#pragma unroll
-    for (int k = 1; k < 32; k <<= 1) {
-      const int u = __shfl_up_sync(0xffffffffu, x, k);
-      if (lane >= k) x += u;
-    }
-    s_warp[lane] = x;
-  }
-  __syncthreads();
-  *total = s_warp[31];
-  return v + (w ? s_warp[w - 1] : 0);
+// Key tiles (units) of the tile whose first token is t0; at least one, in which rows that see
+// nothing get their zeros.
+__device__ __forceinline__ int tile_units(int t0, int tokens, const Seq& s, int block) {
+  return max(1, tiles_seen(min(t0 + tokens, s.ql) - 1, s, block));
 }
 
-// tokens: of a tile (all chains); ctas: of the tile kernel; min_piece: a piece's least key tiles.
-__global__ void __launch_bounds__(kPlanThreads) seq_plan_kernel(SeqAttnArgs a, SeqScratch sc,
-                                                                int tokens, int ctas,
-                                                                int min_piece) {
-  __shared__ int s_warp[32], s_hist[kBuckets], s_slots, s_splits;
-  __shared__ unsigned long long s_work;
-  pdl_launch_dependents();
-  const int tid = threadIdx.x;
-  if (tid == 0) {
-    s_work = 0;
-    s_slots = s_splits = 0;
-    sc.tile_off[0] = 0;
+// ------------------------------------------------------------------ runs of units
+// An item costs about as much as this many units on top of its own (its Q, first scores and
+// epilogue, which the other chains hide only in part).
+constexpr int kItemCost = 4;
+
+// A CTA's run: the first segment, and its extent in units, kItemCost for every item begun included.
+struct Run {
+  int b, t0, h, j0;
+  long long units;
+};
+
+// A segment of a run: key tiles [j0, j0 + nk) of tile (b, t0) and kv head h, of `all`; the part-th
+// of the run.  nk < 0: no more.
+struct Item {
+  int b, t0, h, j0, nk, all, q0, ql, kl, part;
+};
+// Items in flight between the producer and the epilogues: the producer writes item i + 2 when every
+// warp has begun item i, and item i + 4 when they have begun i + 2, i.e. after i's epilogue.
+constexpr int kItemRing = 4;
+
+// The segments of a run, one after another.
+struct Walk {
+  Item it;
+  long long left;  // extent from this segment on
+  int here;        // this segment's extent, were its item not cut
+
+  __device__ __forceinline__ void load(const SeqAttnArgs& a) {
+    const Seq s = load_seq(a, it.b);
+    it.q0 = s.q0;
+    it.ql = s.ql;
+    it.kl = s.kl;
   }
-  if (tid < kBuckets) s_hist[tid] = 0;
-  int n_tiles = 0;
-  for (int base = 0; base < a.B; base += kPlanThreads) {
-    const int b = base + tid;
-    const int n = b < a.B ? ceil_div(load_seq(a, b).ql, tokens) : 0;
-    int total;
-    const int before = block_scan(n, s_warp, &total);
-    if (b < a.B) sc.tile_off[b + 1] = n_tiles + before;
-    n_tiles += total;
+  __device__ __forceinline__ void set(const SeqAttnArgs& a, int tokens) {
+    it.all = tile_units(it.t0, tokens, Seq{it.q0, it.ql, it.kl}, a.block);
+    const int cost = it.j0 == 0 ? kItemCost : 0;
+    here = it.all - it.j0 + cost;
+    it.nk = left >= here ? it.all - it.j0 : (int)left - cost;
   }
-  __syncthreads();
-  // Tile w: sequence b, first token t0, key tiles nk.
-  auto tile = [&](int w, int* b, int* t0, Seq* s) {
-    *b = seq_of_token(sc.tile_off, a.B, w);
-    *s = load_seq(a, *b);
-    *t0 = (w - sc.tile_off[*b]) * tokens;
-    return tiles_seen(min(*t0 + tokens, s->ql) - 1, *s, a.block);
-  };
-  int b, t0;
-  Seq s;
-  unsigned long long work = 0;
-  for (int w = tid; w < n_tiles; w += kPlanThreads) work += tile(w, &b, &t0, &s);
-#pragma unroll
-  for (int k = 16; k > 0; k >>= 1) work += __shfl_xor_sync(0xffffffffu, work, k);
-  if (lane_id() == 0) atomicAdd(&s_work, work);
-  __syncthreads();
-  const unsigned long long share = (s_work * a.Hkv + 2 * ctas - 1) / (2 * ctas);
-  const int piece = (int)max((unsigned long long)min_piece, share);
-  // Pieces of n tiles each (or one less), longest first.
-  auto bucket = [&](int nk, int np) {
-    return kBuckets - 1 - (int)((long long)ceil_div(nk, np) * (kBuckets - 1) / piece);
-  };
-  for (int w = tid; w < n_tiles; w += kPlanThreads) {
-    const int nk = tile(w, &b, &t0, &s), np = max(1, ceil_div(nk, piece));
-    atomicAdd(&s_hist[bucket(nk, np)], np);
-  }
-  __syncthreads();
-  int total;
-  const int mine = tid < kBuckets ? s_hist[tid] : 0;
-  const int before = block_scan(mine, s_warp, &total) - mine;
-  __syncthreads();
-  if (tid < kBuckets) s_hist[tid] = before;
-  __syncthreads();
-  for (int w = tid; w < n_tiles; w += kPlanThreads) {
-    const int nk = tile(w, &b, &t0, &s), np = max(1, ceil_div(nk, piece));
-    const int at = atomicAdd(&s_hist[bucket(nk, np)], np);
-    int slot = -1;
-    if (np > 1) {
-      slot = atomicAdd(&s_slots, np);
-      const int r = atomicAdd(&s_splits, 1);
-      sc.splits[2 * r] = make_int4(s.q0, t0, s.ql, s.kl);
-      sc.splits[2 * r + 1] = make_int4(slot, np, 0, 0);
-    }
-    for (int i = 0; i < np; ++i) {
-      const int j0 = (int)((long long)i * nk / np), j1 = (int)((long long)(i + 1) * nk / np);
-      sc.items[2 * (at + i)] = make_int4(b, t0, j0, j1 - j0);
-      sc.items[2 * (at + i) + 1] = make_int4(slot < 0 ? -1 : slot + i, s.q0, s.ql, s.kl);
+  __device__ __forceinline__ void start(const SeqAttnArgs& a, const Run& r, int tokens) {
+    it.b = r.b;
+    it.t0 = r.t0;
+    it.h = r.h;
+    it.j0 = r.j0;
+    it.part = 0;
+    left = r.units;
+    if (left > 0) {
+      load(a);
+      set(a, tokens);
+      if (it.nk == 0) {  // from the next item on
+        next(a, tokens);
+        it.part = 0;
+      }
     }
   }
-  __syncthreads();
-  if (tid == 0) {
-    sc.head[kPlanItems] = total;
-    sc.head[kPlanSplits] = s_splits;
+  // The next segment: next kv head, next tile, next sequence that has new tokens.
+  __device__ __forceinline__ void next(const SeqAttnArgs& a, int tokens) {
+    left -= here;
+    ++it.part;
+    if (left <= 0) return;
+    it.j0 = 0;
+    if (++it.h == a.Hkv) {
+      it.h = 0;
+      it.t0 += tokens;
+      if (it.t0 >= it.ql) {
+        it.t0 = 0;
+        do {
+          ++it.b;
+          load(a);
+        } while (it.ql == 0);
+      }
+    }
+    set(a, tokens);
   }
-}
+};
 
 // ------------------------------------------------------------------ tile kernel
 template <int D>
 struct Cfg {
   static constexpr int kChains = seq_chains(D);
   static constexpr int kHalves = D / 64;               // 64-channel (128-byte) column blocks
-  static constexpr int kStages = 512 / kBN / kHalves;  // 64 KB of K and 64 KB of V
+  static constexpr int kStages = D == 64 ? 8 : 3;      // of 64 keys: 128 / 96 KB of K and V
   static constexpr int kThreads = 128 + 128 * kChains;
   static constexpr int kCtrlRegs = kChains == 3 ? 56 : 80;
   static constexpr int kSoftRegs = kChains == 3 ? 152 : 208;
@@ -176,41 +149,86 @@ struct Cfg {
 template <int D>
 struct TileSmem {
   using C = Cfg<D>;
-  uint16_t q[C::kChains][C::kHalves][kBM * 64];
+  uint16_t q[2][C::kChains][C::kHalves][kBM * 64];  // this item's and the next one's
   uint16_t k[C::kStages][C::kHalves][kBN * 64];
   uint16_t v[C::kStages][C::kHalves][kBN * 64];
-  uint64_t q_full, q_empty;
+  uint64_t q_full[2], q_empty[2];
   uint64_t k_full[C::kStages], v_full[C::kStages], kv_empty[C::kStages];
   uint64_t s_full[C::kChains], s_empty[C::kChains], p_full[C::kChains], o_bar[C::kChains],
       o_empty[C::kChains], drain[C::kChains];
   uint32_t tmem_base;
   int abort_flag;
   int nonfinite;  // some visible V of a masked tile was not finite
+  Run run;
+  Item item[kItemRing];  // published by the producer with q_full
 };
 
-struct Item {
-  int b, t0, j0, nk, slot, q0, ql, kl, h;
-};
-
-__device__ __forceinline__ Item load_item(const SeqScratch& sc, int idx, int Hkv) {
-  const int e = idx / Hkv;
-  const int4 x = sc.items[2 * e], y = sc.items[2 * e + 1];
-  Item it;
-  it.b = x.x;
-  it.t0 = x.y;
-  it.j0 = x.z;
-  it.nk = x.w;
-  it.slot = y.x;
-  it.q0 = y.y;
-  it.ql = y.z;
-  it.kl = y.w;
-  it.h = idx - e * Hkv;
-  return it;
+// Inclusive scan of v over the CTA's threads; *total: the sum.  s_warp: one value per warp.
+__device__ __forceinline__ long long cta_scan(long long v, long long* s_warp, long long* total) {
+  const int lane = lane_id(), w = warp_id(), n = blockDim.x / 32;
+#pragma unroll
+  for (int k = 1; k < 32; k <<= 1) {
+    const long long u = __shfl_up_sync(0xffffffffu, v, k);
+    if (lane >= k) v += u;
+  }
+  __syncthreads();
+  if (lane == 31) s_warp[w] = v;
+  __syncthreads();
+  long long t = 0;
+  for (int i = 0; i < n; ++i) {
+    if (i == w) v += t;
+    t += s_warp[i];
+  }
+  *total = t;
+  return v;
 }
 
-// The n-th item of this CTA (see the top): c, 2 P - 1 - c, 2 P + c, 4 P - 1 - c, ...
-__device__ __forceinline__ int item_index(int n, int cta, int P) {
-  return n * P + ((n & 1) ? P - 1 - cta : cta);
+// The units of all tiles in order, summed up tile by tile: fn(b, t0, seq, extent of an item, extent
+// before the tile) for every tile, each on one thread.  Returns the total.  Called by all threads;
+// s_seq, s_off: scratch for blockDim sequences.
+template <class Fn>
+__device__ __forceinline__ long long scan_tiles(const SeqAttnArgs& a, int tokens, int4* s_seq,
+                                                long long* s_warp, Fn fn) {
+  const int tid = threadIdx.x, n = blockDim.x;
+  long long before = 0;
+  for (int b0 = 0; b0 < a.B; b0 += n) {
+    Seq s{0, 0, 0};
+    if (b0 + tid < a.B) s = load_seq(a, b0 + tid);
+    long long tiles;
+    const long long end = cta_scan(ceil_div(s.ql, tokens), s_warp, &tiles);
+    s_seq[tid] = make_int4(s.q0, s.ql, s.kl, (int)end);  // .w: tiles up to this sequence's last
+    __syncthreads();
+    for (int w0 = 0; w0 < tiles; w0 += n) {
+      const int w = w0 + tid;
+      int lo = 0, t0 = 0;
+      long long u = 0;
+      if (w < tiles) {
+        int hi = min(n, a.B - b0) - 1;  // the first sequence with .w > w
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          if (s_seq[mid].w > w)
+            hi = mid;
+          else
+            lo = mid + 1;
+        }
+        const int4 x = s_seq[lo];
+        s = Seq{x.x, x.y, x.z};
+        t0 = (w - (x.w - ceil_div(x.y, tokens))) * tokens;
+        u = tile_units(t0, tokens, s, a.block) + kItemCost;
+      }
+      long long total;
+      const long long upto = cta_scan(u * a.Hkv, s_warp, &total);
+      if (u > 0) fn(b0 + lo, t0, s, (int)u, before + upto - u * a.Hkv);
+      before += total;
+    }
+    __syncthreads();
+  }
+  return before;
+}
+
+// Cut x of the units moved to the end of the item [first, first + n) it lies in, if that is near.
+__device__ __forceinline__ long long snap(long long x, long long first, int n, long long near) {
+  return x - first < near ? first : first + n - x < near ? first + n : x;
 }
 
 // Key tiles [j0, j0 + n) of an item that chain c takes (tpt tokens per chain).
@@ -273,6 +291,56 @@ __device__ __forceinline__ void add_nonfinite(const SeqAttnArgs& a, int b, int q
   }
 }
 
+// This CTA's run, into *run (visible after the next barrier), and its entry of the list of cut
+// items: an item whose first part is this run's end.
+__device__ __forceinline__ void find_run(const SeqAttnArgs& a, const SeqScratch& sc, int tokens,
+                                         int4* s_seq, Run* run) {
+  __shared__ long long s_warp[32], s_begin, s_end, s_first;
+  __shared__ int4 s_rec[2];
+  const int P = gridDim.x, cta = blockIdx.x;
+  if (threadIdx.x == 0) {
+    s_rec[0] = make_int4(0, 0, 0, 0);
+  }
+  const long long total = scan_tiles(a, tokens, s_seq, s_warp, [](int, int, const Seq&, int, long long) {});
+  const long long per = (total + P - 1) / P, near = max(per / 16, kItemCost + 4ll);
+  const long long x0 = cta * per, x1 = x0 + per;
+  if (threadIdx.x == 0) {
+    s_begin = min(x0, total);
+    s_end = min(x1, total);
+    run->b = run->t0 = run->h = run->j0 = 0;
+  }
+  scan_tiles(a, tokens, s_seq, s_warp, [&](int b, int t0, const Seq& s, int n, long long before) {
+    const long long end = before + (long long)n * a.Hkv;
+    if (before <= x0 && x0 < end) {
+      const int h = (int)((x0 - before) / n);
+      const long long first = before + (long long)h * n, x = snap(x0, first, n, near);
+      s_begin = x;
+      run->b = b;
+      run->t0 = t0;
+      run->h = h;
+      run->j0 = x == first ? 0 : (int)(x - first) - kItemCost;  // all: from the next item on
+    }
+    if (before <= x1 && x1 < end) {
+      const int h = (int)((x1 - before) / n);
+      const long long first = before + (long long)h * n, x = snap(x1, first, n, near);
+      s_end = x;
+      if (x > first && x < first + n && x0 - first < near) {
+        // The cuts k per of this item that stay: first + near <= k per <= first + n - near.
+        const int last = (int)((first + n - near) / per);
+        s_rec[0] = make_int4(last - cta + 1, h, t0, b);
+        s_rec[1] = make_int4(s.q0, s.ql, s.kl, 0);
+        s_first = first;
+      }
+    }
+  });
+  if (threadIdx.x == 0) {
+    run->units = s_end - s_begin;
+    if (s_rec[0].x) s_rec[1].w = 2 * cta + (s_first > s_begin);  // the first part's slot
+    sc.recs[2 * cta] = s_rec[0];
+    sc.recs[2 * cta + 1] = s_rec[1];
+  }
+}
+
 template <int D, bool F16, bool kPaged>
 __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
     seq_tile_kernel(const __grid_constant__ CUtensorMap tmap_q,
@@ -289,10 +357,14 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
   volatile int* abort_flag = &sm.abort_flag;
   unsigned int* err = prm.err;
   pdl_launch_dependents();
+  find_run(prm, sc, kChains * (kBM / prm.group), reinterpret_cast<int4*>(sm.q), &sm.run);
+  fence_proxy_async_smem();  // sm.q was scratch: before the copies into it
 
   if (threadIdx.x == 0) {
-    mbar_init(&sm.q_full, 1);
-    mbar_init(&sm.q_empty, kChains);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&sm.q_full[s], 1);
+      mbar_init(&sm.q_empty[s], 5 * kChains);  // each chain's MMA warp and softmax warps
+    }
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&sm.k_full[s], 1);
       mbar_init(&sm.v_full[s], 1);
@@ -323,10 +395,9 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, sm.tmem_base, 0);
 
-  pdl_wait();  // the plan
   const int Hkv = prm.Hkv, group = prm.group, block = prm.block;
   const int tpt = kBM / group;  // tokens of a chain
-  const int n_items = sc.head[kPlanItems] * Hkv;
+  const int tokens = kChains * tpt;
 
   if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kCtrlRegs));
   if (warp == 0) {
@@ -336,17 +407,28 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
     const int log2p = prm.kv.log2_page, ps = prm.kv.page_size;
     const int ppt = kPaged ? (ps >= kBN ? 1 : kBN / ps) : 1;  // pages (boxes) of a tile
     const uint32_t box_bytes = (kPaged && ps < kBN ? ps : kBN) * 128;
-    for (int idx; ok && (idx = item_index(ic, cta, P)) < n_items; ++ic) {
-      const Item it = load_item(sc, idx, Hkv);
-      ok = mbar_wait_warp(&sm.q_empty, (ic & 1) ^ 1, err, abort_flag);
+    Walk walk;
+    for (walk.start(prm, sm.run, tokens);; walk.next(prm, tokens), ++ic) {
+      const Item& it = walk.it;
+      const int qb = ic & 1;
+      ok = mbar_wait_warp(&sm.q_empty[qb], ((ic >> 1) & 1) ^ 1, err, abort_flag);
       if (!ok) break;
+      if (walk.left <= 0) {  // the end of the run
+        if (lane == 0) {
+          sm.item[ic % kItemRing].nk = -1;
+          mbar_arrive(&sm.q_full[qb]);
+        }
+        break;
+      }
       const int chains = min(kChains, ceil_div(it.ql - it.t0, tpt));
       if (elect_one()) {
-        mbar_arrive_expect_tx(&sm.q_full, chains * kHalves * tpt * group * 128);
+        sm.item[ic % kItemRing] = it;
+        mbar_arrive_expect_tx(&sm.q_full[qb], chains * kHalves * tpt * group * 128);
         for (int c = 0; c < chains; ++c)
 #pragma unroll
           for (int hf = 0; hf < kHalves; ++hf)
-            tma_load_4d(sm.q[c][hf], &tmap_q, &sm.q_full, hf * 64, 0, it.h, it.q0 + it.t0 + c * tpt);
+            tma_load_4d(sm.q[qb][c][hf], &tmap_q, &sm.q_full[qb], hf * 64, 0, it.h,
+                        it.q0 + it.t0 + c * tpt);
       }
       __syncwarp();
       // Page ids: lane l holds that of page first + l; `next` the 32 after them.
@@ -390,12 +472,12 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
         }
         __syncwarp();
       }
+      if (!ok) break;
     }
     if (!ok && lane == 0) {
       // Let the copies this warp issued land before the CTA releases its shared memory.
-      if (ic > 0)
-        for (int t = 0; t < 1000000 && !mbar_try_wait(&sm.q_full, (ic - 1) & 1); ++t) {}
-      for (int t = 0; t < 1000000 && !mbar_try_wait(&sm.q_full, ic & 1); ++t) {}
+      for (uint32_t i = ic > 2 ? ic - 2 : 0; i <= ic; ++i)
+        for (int t = 0; t < 1000000 && !mbar_try_wait(&sm.q_full[i & 1], (i >> 1) & 1); ++t) {}
       for (int s = 0; s < kStages; ++s) {
         if (lc > (uint32_t)s) {
           const uint32_t last = (lc - 1 - s) / kStages * kStages + s;  // last use of stage s
@@ -410,21 +492,19 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
     const int c = warp - 1;
     const uint32_t id_s = idesc_16bit<F16>(kBM, kBN, 0);  // Q (K-major) x K^T (K-major)
     const uint32_t id_o = idesc_16bit<F16>(kBM, 64, 1);   // P (TMEM) x V (MN-major)
-    const uint64_t dq = sdesc_sw128(smem_u32(sm.q[c][0]));
     const uint32_t t_s = tmem + C::kColS + c * kBN;
     const uint32_t t_o = tmem + C::kColO + c * D;
     const uint32_t t_p = tmem + C::kColP + c * (kBN / 2);
     uint32_t lc = 0, ic = 0, g = 0, oc = 0;  // ring tiles, items, this chain's tiles, its items
     bool ok = true;
-    Item it;
-    int idx = item_index(0, cta, P);
-    if (idx < n_items) it = load_item(sc, idx, Hkv);
-    for (; ok && idx < n_items; ++ic) {
-      const int nk = it.nk, n = chain_tiles(it, c, tpt, block);
-      idx = item_index(ic + 1, cta, P);
-      if (idx < n_items) it = load_item(sc, idx, Hkv);  // ahead of its use
-      ok = mbar_wait_warp(&sm.q_full, ic & 1, err, abort_flag);
+    for (;; ++ic) {
+      const int qb = ic & 1;
+      ok = mbar_wait_warp(&sm.q_full[qb], (ic >> 1) & 1, err, abort_flag);
       if (!ok) break;
+      const Item& it = sm.item[ic % kItemRing];
+      const int nk = it.nk, n = nk < 0 ? 0 : chain_tiles(it, c, tpt, block);
+      if (nk < 0) break;
+      const uint64_t dq = sdesc_sw128(smem_u32(sm.q[qb][c][0]));
       tc_fence_after();
       const uint32_t lc0 = lc, g0 = g;
       auto issue_s = [&](int j) -> bool {
@@ -440,7 +520,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
             tc_mma_ss(t_s, dq + (kk >> 2) * (kBM * 128 / 16) + 2 * (kk & 3),
                       dk + (kk >> 2) * (kBN * 128 / 16) + 2 * (kk & 3), id_s, kk > 0);
           tc_commit(&sm.s_full[c]);
-          if (j == n - 1) tc_commit(&sm.q_empty);
+          if (j == n - 1) tc_commit(&sm.q_empty[qb]);
         }
         __syncwarp();
         return true;
@@ -448,7 +528,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       if (n > 0) {
         ok = issue_s(0);
       } else if (lane == 0) {
-        mbar_arrive(&sm.q_empty);
+        mbar_arrive(&sm.q_empty[qb]);
       }
       for (int j = 0; j < n && ok; ++j) {
         if (j + 1 < n) {
@@ -483,6 +563,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
              mbar_wait_warp(&sm.v_full[st], (l / kStages) & 1, err, abort_flag);
         if (ok && lane == 0) mbar_arrive(&sm.kv_empty[st]);
       }
+      if (!ok) break;
       lc = lc0 + nk;
       g = g0 + n;
       oc += n > 0;
@@ -509,8 +590,13 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
     const float cs = fmaxf(fabsf(prm.scale_log2), 1e-30f);
     uint32_t g = 0, lc = 0;
     bool ok = true;
-    for (int n_it = 0, idx; ok && (idx = item_index(n_it, cta, P)) < n_items; ++n_it) {
-      const Item it = load_item(sc, idx, Hkv);
+    for (uint32_t ic = 0;; ++ic) {
+      ok = mbar_wait_warp(&sm.q_full[ic & 1], (ic >> 1) & 1, err, abort_flag);
+      if (!ok) break;
+      const Item& it = sm.item[ic % kItemRing];
+      if (it.nk < 0) break;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.q_empty[ic & 1]);  // seen: its q_full may move on
       const int n = chain_tiles(it, c, tpt, block);
       const int tok = it.t0 + c * tpt + row_tok;  // this thread's token in its sequence
       const bool valid = row_tok < tpt && tok < it.ql;
@@ -519,27 +605,19 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       const int masked_from = max(row_limit(it.t0, it.ql, it.kl, block), 0) / kBN;
       const bool active = __any_sync(0xffffffffu, valid);
       float m = kUnset, lsum = 0.f;
-      for (int jj = 0; jj < n; ++jj, ++g) {
-        const int j = it.j0 + jj;
-        const bool masked = j >= masked_from;  // uniform over the chain
-        ok = mbar_wait_warp(&sm.s_full[c], g & 1, err, abort_flag);
-        if (!ok) break;
-        if (masked) {
+      // One key tile; kMasked: some row of the item does not see all of it (uniform over the
+      // chains), or the scores are negated.
+      auto tile = [&](auto masked_const, int jj) -> bool {
+        constexpr bool kMasked = decltype(masked_const)::value;
+        if (!mbar_wait_warp(&sm.s_full[c], g & 1, err, abort_flag)) return false;
+        if (kMasked) {
           const uint32_t l = lc + jj;
           const int st = l % kStages;
-          ok = mbar_wait_warp(&sm.v_full[st], (l / kStages) & 1, err, abort_flag);
-          if (!ok) break;
-          scrub_v<D, F16>(sm.v[st][0], it.kl - j * kBN, row, &sm.nonfinite);
+          if (!mbar_wait_warp(&sm.v_full[st], (l / kStages) & 1, err, abort_flag)) return false;
+          if (it.j0 + jj >= masked_from)
+            scrub_v<D, F16>(sm.v[st][0], it.kl - (it.j0 + jj) * kBN, row, &sm.nonfinite);
         }
         tc_fence_after();
-        if (!active) {  // no row of this warp exists: its lanes of P and O are never read
-          tc_fence_before();
-          mbar_arrive(&sm.s_empty[c]);
-          if (g > 0) ok = mbar_wait_warp(&sm.o_bar[c], (g - 1) & 1, err, abort_flag);
-          if (!ok) break;
-          mbar_arrive(&sm.p_full[c]);
-          continue;
-        }
         float s[kBN], pmx[kBN / 32];
 #pragma unroll
         for (int cc = 0; cc < kBN / 32; ++cc) tmem_ld32_max(t_s + 32 * cc, s + 32 * cc, pmx[cc]);
@@ -547,8 +625,8 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
         tc_fence_before();
         mbar_arrive(&sm.s_empty[c]);  // the MMA warp may overwrite S_c now
         float mx = fmaxf(pmx[0], pmx[1]);
-        if (masked || flip) {
-          const int n_seen = lim - j * kBN;
+        if (kMasked) {
+          const int n_seen = lim - (it.j0 + jj) * kBN;
 #pragma unroll
           for (int i = 0; i < kBN; ++i) {
             if (flip) s[i] = -s[i];
@@ -592,8 +670,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
         lsum = lsum * alpha + (at.x + at.y);
         // P_c and O_c are free once P_c(g-1) V has completed.
         if (g > 0) {
-          ok = mbar_wait_warp(&sm.o_bar[c], (g - 1) & 1, err, abort_flag);
-          if (!ok) break;
+          if (!mbar_wait_warp(&sm.o_bar[c], (g - 1) & 1, err, abort_flag)) return false;
           tc_fence_after();
         }
 #pragma unroll
@@ -612,6 +689,29 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive(&sm.p_full[c]);
+        ++g;
+        return true;
+      };
+      if (active) {
+        const int clear = flip ? 0 : min(max(masked_from - it.j0, 0), n);
+        int jj = 0;
+        for (; jj < clear && ok; ++jj) ok = tile(std::false_type{}, jj);
+        for (; jj < n && ok; ++jj) ok = tile(std::true_type{}, jj);
+      } else {
+        // No row of this warp exists: its lanes of P and O are never read.
+        for (int jj = 0; jj < n && ok; ++jj, ++g) {
+          const uint32_t l = lc + jj;
+          const int st = l % kStages, j = it.j0 + jj;
+          ok = mbar_wait_warp(&sm.s_full[c], g & 1, err, abort_flag);
+          if (ok && j >= masked_from) {
+            ok = mbar_wait_warp(&sm.v_full[st], (l / kStages) & 1, err, abort_flag);
+            if (ok) scrub_v<D, F16>(sm.v[st][0], it.kl - j * kBN, row, &sm.nonfinite);
+          }
+          if (!ok) break;
+          mbar_arrive(&sm.s_empty[c]);
+          if (g > 0) ok = mbar_wait_warp(&sm.o_bar[c], (g - 1) & 1, err, abort_flag);
+          if (ok) mbar_arrive(&sm.p_full[c]);
+        }
       }
       if (!ok) break;
       lc += it.nk;
@@ -623,8 +723,8 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       }
       const bool refill = n > 0 && *(volatile int*)&sm.nonfinite != 0;
       const int head = it.h * group + row_head;
-      if (it.slot >= 0) {  // a piece: unnormalised O, m and l
-        const size_t r = ((size_t)(it.slot * Hkv + it.h) * kChains + c) * kBM + row;
+      if (it.nk < it.all) {  // a part: unnormalised O, m and l
+        const size_t r = ((size_t)(2 * cta + (it.part > 0)) * kChains + c) * kBM + row;
 #pragma unroll
         for (int q = 0; q < D / 32; ++q) {
           if (n == 0) break;
@@ -688,78 +788,17 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
   }
 }
 
-// ------------------------------------------------------------------ pieces joined
-constexpr int kCombineThreads = 256;
-
-// One warp per row of a cut tile: M = max m_i, o = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i.
-template <int D, bool F16>
-__global__ void __launch_bounds__(kCombineThreads) seq_combine_kernel(SeqAttnArgs a, SeqScratch sc) {
-  constexpr int kChains = seq_chains(D), kRows = kChains * kBM, kPer = D / 32;
-  pdl_wait();
-  const int n_splits = sc.head[kPlanSplits], Hkv = a.Hkv, tpt = kBM / a.group;
-  const int lane = lane_id();
-  const long long rows = (long long)n_splits * Hkv * kRows;
-  const long long step = (long long)gridDim.x * (kCombineThreads / 32);
-  for (long long w = (long long)blockIdx.x * (kCombineThreads / 32) + warp_id(); w < rows; w += step) {
-    const int r = (int)(w % kRows), sh = (int)(w / kRows), h = sh % Hkv, sp = sh / Hkv;
-    const int row = r % kBM, row_tok = row / a.group;
-    const int4 x = sc.splits[2 * sp], y = sc.splits[2 * sp + 1];
-    const int tok = x.y + (r / kBM) * tpt + row_tok;
-    if (row_tok >= tpt || tok >= x.z) continue;
-    const size_t pitch = (size_t)Hkv * kRows;  // rows between pieces
-    const size_t r0 = ((size_t)y.x * Hkv + h) * kRows + r;
-    const int np = y.y;
-    float M = kUnset;
-    for (int i = lane; i < np; i += 32) M = fmaxf(M, sc.part_ml[r0 + i * pitch].x);
-#pragma unroll
-    for (int k = 16; k > 0; k >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, k));
-    float L = 0.f, o[kPer];
-#pragma unroll
-    for (int c = 0; c < kPer; ++c) o[c] = 0.f;
-    for (int i0 = 0; i0 < np; i0 += 32) {
-      float2 ml = make_float2(kUnset, 0.f);
-      if (i0 + lane < np) ml = sc.part_ml[r0 + (i0 + lane) * pitch];
-      const float wgt = fast_exp2(ml.x - M);
-      const int n = min(32, np - i0);
-#pragma unroll 4
-      for (int i = 0; i < n; ++i) {
-        const float l = __shfl_sync(0xffffffffu, ml.y, i), f = __shfl_sync(0xffffffffu, wgt, i);
-        if (l == 0.f) continue;  // nothing visible in this piece (its O may be unwritten)
-        L = fmaf(f, l, L);
-        const float* src = sc.part_o + (r0 + (i0 + i) * pitch) * D + lane * kPer;
-#pragma unroll
-        for (int c = 0; c < kPer; ++c) o[c] = fmaf(f, src[c], o[c]);
-      }
-    }
-    const int lim = row_limit(tok, x.z, x.w, a.block);
-    const float inv = 1.f / L;
-    const int head = h * a.group + row - row_tok * a.group;
-    uint16_t* out = a.out + (int64_t)(x.x + tok) * a.out_stride + head * D + lane * kPer;
-#pragma unroll
-    for (int c = 0; c < kPer; c += 2)
-      *reinterpret_cast<uint32_t*>(out + c) =
-          lim > 0 ? pack2<F16>(o[c] * inv, o[c + 1] * inv) : 0u;
-    if (a.lse && lane == 0)
-      a.lse[(size_t)(x.x + tok) * a.Hq + head] =
-          lim > 0 ? (M + log2f(L)) * 0.69314718055994531f : -INFINITY;
-  }
-}
-
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 struct ScratchLayout {
-  size_t items, splits, tile_off, part_ml, part_o, end;
+  size_t part_ml, part_o, end;
 };
-ScratchLayout scratch_layout(int d, int Hq, int Hkv, int64_t T, int64_t B) {
-  const int chains = seq_chains(d), tokens = chains * (kBM / (Hq / Hkv));
-  const int64_t tiles = T / tokens + B;  // sum of ceil(n / tokens)
+ScratchLayout scratch_layout(int d) {
+  const size_t rows = (size_t)kMaxSlots * seq_chains(d) * kBM;
   ScratchLayout l;
-  l.items = 512;  // after the error word and the counts
-  l.splits = l.items + align256((size_t)(tiles + kMaxSlots) * 2 * sizeof(int4));
-  l.tile_off = l.splits + align256((size_t)kMaxSlots * 2 * sizeof(int4));
-  l.part_ml = l.tile_off + align256((size_t)(B + 1) * sizeof(int));
-  l.part_o = l.part_ml + align256((size_t)kMaxSlots * chains * kBM * sizeof(float2));
-  l.end = l.part_o + align256((size_t)kMaxSlots * chains * kBM * d * sizeof(float));
+  l.part_ml = 256 + align256((size_t)kMaxRecs * 2 * sizeof(int4));  // after the error word and the list
+  l.part_o = l.part_ml + align256(rows * sizeof(float2));
+  l.end = l.part_o + align256(rows * d * sizeof(float));
   return l;
 }
 
@@ -781,27 +820,17 @@ cudaError_t launch_tiles(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms
   const void* tile = reinterpret_cast<const void*>(seq_tile_kernel<D, F16, kPaged>);
   e = cudaFuncSetAttribute(tile, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  // A piece has at least 16 tiles (1,024 keys): below that its start and its join outweigh it.
-  seq_plan_kernel<<<1, kPlanThreads, 0, st>>>(a, sc, C::kChains * tpt, P, 16);
+  seq_tile_kernel<D, F16, kPaged><<<P, C::kThreads, smem, st>>>(mq, mk, mv, a, sc);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  SeqAttnArgs aa = a;
-  SeqScratch ss = sc;
-  void* targs[] = {&mq, &mk, &mv, &aa, &ss};
-  e = launch_pdl(tile, P, C::kThreads, smem, st, targs);
-  if (e != cudaSuccess) return e;
-  void* cargs[] = {&aa, &ss};
-  prof_extra_launch();
-  prof_extra_launch();
-  return launch_pdl(reinterpret_cast<const void*>(seq_combine_kernel<D, F16>), 2 * P, kCombineThreads, 0,
-                    st, cargs);
+  return launch_seq_join(a, sc, true, P, st);
 }
 
 }  // namespace
 
-cudaError_t launch_pdl(const void* fn, int grid, int threads, int smem, cudaStream_t st, void** args) {
+cudaError_t launch_pdl(const void* fn, dim3 grid, int threads, int smem, cudaStream_t st, void** args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
@@ -831,18 +860,13 @@ cudaError_t make_kv_maps(const SeqAttnArgs& a, int tile_keys, CUtensorMap* mk, C
   return e != cudaSuccess ? e : make_tmap_16bit_4d(mv, a.v, a.fp16 != 0, dims, vs, box);
 }
 
-size_t seq_scratch_bytes(int d, int Hq, int Hkv, int64_t T, int64_t B) {
-  return scratch_layout(d, Hq, Hkv, T, B).end;
-}
+size_t seq_scratch_bytes(int d) { return scratch_layout(d).end; }
 
-SeqScratch carve_seq_scratch(void* ws, int d, int Hq, int Hkv, int64_t T, int64_t B) {
-  const ScratchLayout l = scratch_layout(d, Hq, Hkv, T, B);
+SeqScratch carve_seq_scratch(void* ws, int d) {
+  const ScratchLayout l = scratch_layout(d);
   char* p = static_cast<char*>(ws);
   SeqScratch s;
-  s.head = reinterpret_cast<int*>(p + 256);
-  s.items = reinterpret_cast<int4*>(p + l.items);
-  s.splits = reinterpret_cast<int4*>(p + l.splits);
-  s.tile_off = reinterpret_cast<int*>(p + l.tile_off);
+  s.recs = reinterpret_cast<int4*>(p + 256);
   s.part_ml = reinterpret_cast<float2*>(p + l.part_ml);
   s.part_o = reinterpret_cast<float*>(p + l.part_o);
   return s;

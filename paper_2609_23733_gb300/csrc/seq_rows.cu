@@ -9,8 +9,7 @@
 // The work is the sequence of units (sequence, kv head, 16 rows, 64 keys); CTA c of P takes
 // the units [c u, (c + 1) u), whatever items they belong to, so that all CTAs end together
 // for any mix of lengths; an item (16 rows of a kv head) that a CTA holds in part leaves a
-// partial result, and seq_rows_combine_kernel (a programmatic dependent launch) joins the
-// parts in order.  Each CTA finds its place by a scan over the sequences' lengths.
+// partial result, and seq_join_kernel (a programmatic dependent launch) joins the parts in order.  Each CTA finds its place by a scan over the sequences' lengths.
 //   warp 4      TMA: K / V tiles through a ring, page by page (page ids read 32 ahead).
 //   warps 0-3   16 keys of every tile each: S = Q K^T (16 x 16), softmax against the warp's own
 //               running maximum (moved when it grows by more than 2^8), O += P V in registers;
@@ -63,7 +62,7 @@ struct Place {
 __device__ __forceinline__ void fill_place(const SeqAttnArgs& a, int b, Place* p) {
   p->b = b;
   p->s = load_seq(a, b);
-  p->n_kv = (int)(((long long)p->s.kl + kBN - 1) / kBN);
+  p->n_kv = max(1, (int)(((long long)p->s.kl + kBN - 1) / kBN));  // one even without keys: for the zeros
   p->n_rt = (int)(((long long)p->s.ql * a.group + kRows - 1) / kRows);
 }
 
@@ -219,22 +218,12 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
     tma_prefetch_desc(&tmap_v);
   }
   const int Hkv = prm.Hkv, group = prm.group, block = prm.block;
-  // Rows of sequences without keys: nothing below writes them.
   long long mine = 0;
   for (int b = tid; b < prm.B; b += kThreads) mine += seq_units(prm, b);
-  for (int b = cta; b < prm.B; b += P) {
-    const Seq s = load_seq(prm, b);
-    if (s.kl > 0) continue;
-    for (long long r = tid; r < (long long)s.ql * prm.Hq; r += kThreads) {
-      const int t = s.q0 + (int)(r / prm.Hq), h = (int)(r % prm.Hq);
-      uint4* out = reinterpret_cast<uint4*>(prm.out + t * prm.out_stride + h * D);
-      for (int c = 0; c < D / 8; ++c) out[c] = make_uint4(0, 0, 0, 0);
-      if (prm.lse) prm.lse[(size_t)t * prm.Hq + h] = -INFINITY;
-    }
-  }
   const long long total = cta_sum(mine, scratch);  // its barriers also publish the mbarriers
   const long long per = units_per_cta(total, P);
   const long long begin = min(cta * per, total), end = min(begin + per, total);
+  if (tid == 0) sc.recs[2 * cta] = make_int4(0, 0, 0, 0);  // until the producer knows better
   if (begin >= end) return;  // uniform
   Place pl = locate(prm, begin, scratch);
   bool ok = true;
@@ -283,6 +272,14 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
           }
         }
         __syncwarp();
+      }
+      // This CTA's entry of the list of cut items: one whose first part ends this run.
+      if (u + nk == end && lane == 0) {
+        const long long item0 = u - local, item1 = item0 + pl.n_kv;
+        const bool cut = end < item1 && item0 >= begin;
+        const int np = cut ? (int)((item1 - 1) / per) - cta + 1 : 0;
+        sc.recs[2 * cta] = make_int4(np, h, item - h * pl.n_rt, pl.b);
+        sc.recs[2 * cta + 1] = make_int4(pl.s.q0, pl.s.ql, pl.s.kl, 2 * cta + (item0 > begin));
       }
       u += nk;
       if (u < end && u - pl.base >= pl.units(Hkv)) advance(prm, &pl);
@@ -537,94 +534,6 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
   }
 }
 
-// CTA c looks at the boundary between the tile kernel's CTAs c - 1 and c: if it is the first
-// one inside an item, it joins the item's parts, m the maximum, o = sum 2^(m_i - m) o_i / sum
-// 2^(m_i - m) l_i.  The warps share the rows and, per row, the parts (in a fixed order).
-constexpr int kJoinThreads = 1024;
-
-template <int D, bool F16>
-__global__ void __launch_bounds__(kJoinThreads)
-    seq_rows_combine_kernel(const __grid_constant__ SeqAttnArgs a, const SeqScratch sc) {
-  __shared__ long long scratch[33];
-  __shared__ __align__(16) float s_o[32][D];
-  __shared__ __align__(8) float2 s_ml[32];
-  constexpr int kLanes = D / 4, kAtOnce = 32 / kLanes;  // lanes of a row, parts a warp reads at once
-  const int P = gridDim.x + 1, cta = blockIdx.x + 1, tid = threadIdx.x;
-  long long mine = 0;
-  for (int b = tid; b < a.B; b += kJoinThreads) mine += seq_units(a, b);
-  const long long total = cta_sum(mine, scratch), per = units_per_cta(total, P);
-  const long long x = cta * per;
-  // The grid ends after the one ahead of it (whose results later work in the stream reads), even
-  // where there is nothing to join: its first CTA waits.
-  if (cta == 1) pdl_wait();
-  if (x >= total) return;  // uniform
-  const Place pl = locate(a, x, scratch);
-  const int item = (int)((x - pl.base) / pl.n_kv);
-  const long long first = pl.base + (long long)item * pl.n_kv, last = first + pl.n_kv;
-  if (first == x || x - per > first) return;  // not inside the item, or not the first boundary
-  const int h = item / pl.n_rt, rt = item - h * pl.n_rt;
-  const int np = (int)((last - 1) / per) - cta + 2;  // parts: of CTAs c - 1, c, ..
-  const size_t slot0 = 2 * (size_t)(cta - 1) + (first == x - per ? 0 : 1);
-  const int rows = min(kRows, pl.s.ql * a.group - rt * kRows);
-  pdl_wait();  // the parts
-  const int warp = warp_id(), lane = lane_id();
-  const int wpr = rows <= 1 ? 32 : rows <= 2 ? 16 : rows <= 4 ? 8 : rows <= 8 ? 4 : 2;  // warps of a row
-  const int r = warp / wpr, sub = warp - r * wpr;
-  float M = kUnset, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  if (r < rows) {
-    auto slot = [&](int i) { return i == 0 ? slot0 : 2 * (size_t)(cta - 1 + i); };
-    // This warp's share: parts [i0, i1).
-    const int i0 = (int)((long long)sub * np / wpr), i1 = (int)((long long)(sub + 1) * np / wpr);
-    for (int i = i0 + lane; i < i1; i += 32) M = fmaxf(M, sc.part_ml[slot(i) * kRows + r].x);
-#pragma unroll
-    for (int k = 16; k > 0; k >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, k));
-    const int sl = lane / kLanes, c = (lane % kLanes) * 4;
-#pragma unroll 4
-    for (int i = i0 + sl; i < i1; i += kAtOnce) {
-      const size_t row = slot(i) * kRows + r;
-      const float2 ml = sc.part_ml[row];
-      const float4 v = *reinterpret_cast<const float4*>(sc.part_o + row * D + c);
-      const float f = fast_exp2(ml.x - M);
-      L = fmaf(f, ml.y, L);
-      o[0] = fmaf(f, v.x, o[0]);
-      o[1] = fmaf(f, v.y, o[1]);
-      o[2] = fmaf(f, v.z, o[2]);
-      o[3] = fmaf(f, v.w, o[3]);
-    }
-    if (kAtOnce == 2) {
-      L += __shfl_xor_sync(0xffffffffu, L, 16);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] += __shfl_xor_sync(0xffffffffu, o[k], 16);
-    }
-    if (sl == 0) *reinterpret_cast<float4*>(&s_o[warp][c]) = make_float4(o[0], o[1], o[2], o[3]);
-    if (lane == 0) s_ml[warp] = make_float2(M, L);
-  }
-  __syncthreads();
-  for (int rr = warp; rr < rows; rr += 32) {
-    float top = kUnset, sum = 0.f, y[D / 32];
-#pragma unroll
-    for (int c = 0; c < D / 32; ++c) y[c] = 0.f;
-    for (int w = 0; w < wpr; ++w) top = fmaxf(top, s_ml[rr * wpr + w].x);
-    for (int w = 0; w < wpr; ++w) {
-      const float2 ml = s_ml[rr * wpr + w];
-      const float f = fast_exp2(ml.x - top);
-      sum = fmaf(f, ml.y, sum);
-#pragma unroll
-      for (int c = 0; c < D / 32; ++c) y[c] = fmaf(f, s_o[rr * wpr + w][lane * (D / 32) + c], y[c]);
-    }
-    const int row = rt * kRows + rr, tok = row / a.group, head = h * a.group + row - tok * a.group;
-    const int lim = row_limit(tok, pl.s.ql, pl.s.kl, a.block);
-    const float inv = 1.f / sum;
-    uint16_t* out = a.out + (int64_t)(pl.s.q0 + tok) * a.out_stride + head * D + lane * (D / 32);
-#pragma unroll
-    for (int c = 0; c < D / 32; c += 2)
-      *reinterpret_cast<uint32_t*>(out + c) = lim > 0 ? pack2<F16>(y[c] * inv, y[c + 1] * inv) : 0u;
-    if (a.lse && lane == 0)
-      a.lse[(size_t)(pl.s.q0 + tok) * a.Hq + head] =
-          lim > 0 ? (top + log2f(sum)) * 0.69314718055994531f : -INFINITY;
-  }
-}
-
 template <int D, bool F16, bool kPaged>
 cudaError_t launch_rows(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms, cudaStream_t st) {
   using C = RowsCfg<D>;
@@ -639,12 +548,7 @@ cudaError_t launch_rows(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms,
   seq_rows_kernel<D, F16, kPaged><<<P, kThreads, smem, st>>>(mk, mv, a, sc);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  SeqAttnArgs aa = a;
-  SeqScratch ss = sc;
-  void* args[] = {&aa, &ss};
-  prof_extra_launch();
-  return launch_pdl(reinterpret_cast<const void*>(seq_rows_combine_kernel<D, F16>), P - 1, kJoinThreads, 0,
-                    st, args);
+  return launch_seq_join(a, sc, false, P, st);
 }
 
 }  // namespace
