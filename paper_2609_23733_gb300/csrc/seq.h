@@ -42,6 +42,8 @@ cudaError_t launch_rope_append(const RopeAppendArgs& a, int num_sms, cudaStream_
 struct SeqAttnArgs {
   int T, B, Hq, Hkv, group, d, fp16;
   int block;
+  int chain_tokens;          // tokens of a chain (128 / group rows each)
+  int block_chains;          // > 0: chains start anew at every mask block, this many per block
   float scale_log2;          // scale x log2(e)
   const uint16_t* q;
   int64_t q_stride;
@@ -59,10 +61,11 @@ struct SeqAttnArgs {
 
 // Attention's scratch inside the caller's workspace, after the error word.
 struct SeqScratch {
-  int4* recs;       // [CTAs][2] items cut between CTAs: {parts (0: none), kv head, first token or
+  int4* recs;       // [CTAs][2] items cut between CTAs: {parts (0: none), kv head, first chain or
                     // row tile, sequence}, {q0, ql, kl, first part's slot}; part i > 0 lies in slot
                     // 2 (cta + i)
-  float* part_o;    // partial outputs, unnormalised: [slot][rows][d]
+  float* part_o;    // partial outputs, unnormalised: [slot][rows][d], or, of the tile kernel (written
+                    // row by row in parallel), [slot][chain][d / 4][128 rows][4]
   float2* part_ml;  // [slot][rows] (m, l)
 };
 constexpr int kMaxCtas = 160;            // CTAs of the tile kernel, at most (one per SM)
@@ -131,6 +134,27 @@ __device__ __forceinline__ int row_limit(int i, int ql, int kl, int block) {
   return kl - ql + i + min(rest, step);
 }
 
+// The new tokens of a sequence in chains of up to chain_tokens.  Where that wastes little, chains
+// do not run across mask blocks, so that all rows of a chain see the same keys.
+__device__ __forceinline__ int count_chains(const SeqAttnArgs& a, int ql) {
+  const int n = a.chain_tokens;
+  if (a.block_chains == 0) return (int)(((long long)ql + n - 1) / n);
+  const int full = ql / a.block;
+  return full * a.block_chains + (ql - full * a.block + n - 1) / n;
+}
+__device__ __forceinline__ int chain_start(const SeqAttnArgs& a, int chain) {
+  if (a.block_chains == 0) return chain * a.chain_tokens;
+  const int full = chain / a.block_chains;
+  return full * a.block + (chain - full * a.block_chains) * a.chain_tokens;
+}
+// One past the chain's last token.
+__device__ __forceinline__ int chain_end(const SeqAttnArgs& a, int chain, int ql) {
+  const int start = chain_start(a, chain);
+  int end = min(start + a.chain_tokens, ql);
+  if (a.block_chains) end = min(end, (chain / a.block_chains + 1) * a.block);
+  return end;
+}
+
 // The last sequence b < B with cu[b] <= t (0 if there is none): the owner of token t where cu
 // is ascending; always a valid index.
 __device__ __forceinline__ int seq_of_token(const int32_t* cu, int B, int t) {
@@ -179,6 +203,16 @@ __device__ __forceinline__ void tma_load_4d(void* smem_dst, const void* tmap, ui
       "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes"
       " [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(smem_u32(smem_dst)),
       "l"(reinterpret_cast<uint64_t>(tmap)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
+      : "memory");
+}
+
+// 4-D tiled store of a box from shared memory (bulk-group completion).
+__device__ __forceinline__ void tma_store_4d(const void* tmap, const void* smem_src, int x, int y, int z,
+                                             int w) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(
+          reinterpret_cast<uint64_t>(tmap)),
+      "r"(smem_u32(smem_src)), "r"(x), "r"(y), "r"(z), "r"(w)
       : "memory");
 }
 

@@ -21,10 +21,11 @@
 //   warps 4 ..           four softmax warps per chain, a row per thread; the running maximum
 //                        is moved only when it grows by more than 2^8 (exact either way).
 // A chain stops at its own last visible key; the tiles after it are only released.  A tile that
-// some row of the item sees in part takes the masked path: scores past a row's limit become -inf
-// by selection, and V values that are not finite are replaced by 0 in shared memory, since
-// 0 x inf would reach rows that do not see them; rows that do see them get them added back in
-// the epilogue (a flag says whether there were any).
+// some row of the chain does not see in full takes the masked path: scores past a row's limit
+// become -inf by selection, and V values that are not finite are replaced by 0 in shared
+// memory, since 0 x inf would reach rows that do not see them.  Rows that do see them get
+// them added back in the epilogue (a flag says whether there were any), those of the other
+// chains too: adding an infinity or a NaN to a sum that has it already changes nothing.
 // Scores, maxima, sums and outputs are held in 32 bits; P is rounded to the storage type, as the
 // tensor core needs.  Every wait is bounded; a CTA that gives up lets its copies and MMAs land.
 #include <math.h>
@@ -50,84 +51,95 @@ __device__ __forceinline__ int tiles_seen(int token, const Seq& s, int block) {
   return lim > 0 ? ceil_div(lim, kBN) : 0;
 }
 
-// Key tiles (units) of the tile whose first token is t0; at least one, in which rows that see
-// nothing get their zeros.
-__device__ __forceinline__ int tile_units(int t0, int tokens, const Seq& s, int block) {
-  return max(1, tiles_seen(min(t0 + tokens, s.ql) - 1, s, block));
+// Key tiles (units) of the tile that begins with chain c0, kChains at most; at least one, in which
+// rows that see nothing get their zeros.
+template <int kChains>
+__device__ __forceinline__ int tile_units(const SeqAttnArgs& a, int c0, const Seq& s) {
+  const int last = min(c0 + kChains, count_chains(a, s.ql)) - 1;
+  return max(1, tiles_seen(chain_end(a, last, s.ql) - 1, s, a.block));
 }
 
 // ------------------------------------------------------------------ runs of units
 // An item costs about as much as this many units on top of its own (its Q, first scores and
 // epilogue, which the other chains hide only in part).
-constexpr int kItemCost = 4;
+#ifndef VP_SEQ_ITEM_COST
+#define VP_SEQ_ITEM_COST 8
+#endif
+#ifndef VP_Q128
+#define VP_Q128 2
+#endif
+constexpr int kItemCost = VP_SEQ_ITEM_COST;
 
 // A CTA's run: the first segment, and its extent in units, kItemCost for every item begun included.
 struct Run {
-  int b, t0, h, j0;
+  int b, c0, h, j0;
   long long units;
 };
 
-// A segment of a run: key tiles [j0, j0 + nk) of tile (b, t0) and kv head h, of `all`; the part-th
+// A segment of a run: key tiles [j0, j0 + nk) of the tile at chain c0 of sequence b and kv head h, of `all`; the part-th
 // of the run.  nk < 0: no more.
 struct Item {
-  int b, t0, h, j0, nk, all, q0, ql, kl, part;
+  int b, c0, h, j0, nk, all, q0, ql, kl, part;
 };
-// Items in flight between the producer and the epilogues: the producer writes item i + 2 when every
-// warp has begun item i, and item i + 4 when they have begun i + 2, i.e. after i's epilogue.
+// Items in flight between the producer and the epilogues: with two Q buffers, the producer writes
+// item i + 2 after item i's epilogue.
 constexpr int kItemRing = 4;
 
 // The segments of a run, one after another.
+template <int kChains>
 struct Walk {
   Item it;
   long long left;  // extent from this segment on
   int here;        // this segment's extent, were its item not cut
+  int n_chains;    // of the sequence
 
   __device__ __forceinline__ void load(const SeqAttnArgs& a) {
     const Seq s = load_seq(a, it.b);
     it.q0 = s.q0;
     it.ql = s.ql;
     it.kl = s.kl;
+    n_chains = count_chains(a, s.ql);
   }
-  __device__ __forceinline__ void set(const SeqAttnArgs& a, int tokens) {
-    it.all = tile_units(it.t0, tokens, Seq{it.q0, it.ql, it.kl}, a.block);
+  __device__ __forceinline__ void set(const SeqAttnArgs& a) {
+    it.all = tile_units<kChains>(a, it.c0, Seq{it.q0, it.ql, it.kl});
     const int cost = it.j0 == 0 ? kItemCost : 0;
     here = it.all - it.j0 + cost;
     it.nk = left >= here ? it.all - it.j0 : (int)left - cost;
   }
-  __device__ __forceinline__ void start(const SeqAttnArgs& a, const Run& r, int tokens) {
+  __device__ __forceinline__ void start(const SeqAttnArgs& a, const Run& r) {
     it.b = r.b;
-    it.t0 = r.t0;
+    it.c0 = r.c0;
     it.h = r.h;
     it.j0 = r.j0;
     it.part = 0;
     left = r.units;
     if (left > 0) {
       load(a);
-      set(a, tokens);
+      set(a);
       if (it.nk == 0) {  // from the next item on
-        next(a, tokens);
+        next(a);
         it.part = 0;
       }
     }
   }
   // The next segment: next kv head, next tile, next sequence that has new tokens.
-  __device__ __forceinline__ void next(const SeqAttnArgs& a, int tokens) {
+  __device__ __forceinline__ void next(const SeqAttnArgs& a) {
     left -= here;
     ++it.part;
     if (left <= 0) return;
     it.j0 = 0;
     if (++it.h == a.Hkv) {
       it.h = 0;
-      it.t0 += tokens;
-      if (it.t0 >= it.ql) {
-        it.t0 = 0;
+      it.c0 += kChains;
+      if (it.c0 >= n_chains) {
+        it.c0 = 0;
         do {
           ++it.b;
           load(a);
         } while (it.ql == 0);
       }
     }
-    set(a, tokens);
+    set(a);
   }
 };
 
@@ -136,7 +148,8 @@ template <int D>
 struct Cfg {
   static constexpr int kChains = seq_chains(D);
   static constexpr int kHalves = D / 64;               // 64-channel (128-byte) column blocks
-  static constexpr int kStages = D == 64 ? 8 : 3;      // of 64 keys: 128 / 96 KB of K and V
+  static constexpr int kQBufs = D == 64 ? 2 : VP_Q128;
+  static constexpr int kStages = D == 64 ? 8 : (VP_Q128 == 2 ? 3 : 5);      // of 64 keys: 128 / 96 KB of K and V
   static constexpr int kThreads = 128 + 128 * kChains;
   static constexpr int kCtrlRegs = kChains == 3 ? 56 : 80;
   static constexpr int kSoftRegs = kChains == 3 ? 152 : 208;
@@ -149,16 +162,16 @@ struct Cfg {
 template <int D>
 struct TileSmem {
   using C = Cfg<D>;
-  uint16_t q[2][C::kChains][C::kHalves][kBM * 64];  // this item's and the next one's
+  uint16_t q[C::kQBufs][C::kChains][C::kHalves][kBM * 64];  // this item's and the next one's
   uint16_t k[C::kStages][C::kHalves][kBN * 64];
   uint16_t v[C::kStages][C::kHalves][kBN * 64];
-  uint64_t q_full[2], q_empty[2];
+  uint64_t q_full[C::kQBufs], q_empty[C::kQBufs];
   uint64_t k_full[C::kStages], v_full[C::kStages], kv_empty[C::kStages];
   uint64_t s_full[C::kChains], s_empty[C::kChains], p_full[C::kChains], o_bar[C::kChains],
       o_empty[C::kChains], drain[C::kChains];
   uint32_t tmem_base;
   int abort_flag;
-  int nonfinite;  // some visible V of a masked tile was not finite
+  int nonfinite[2];  // V values of masked tiles replaced by 0: any, and any that some row sees
   Run run;
   Item item[kItemRing];  // published by the producer with q_full
 };
@@ -183,24 +196,24 @@ __device__ __forceinline__ long long cta_scan(long long v, long long* s_warp, lo
   return v;
 }
 
-// The units of all tiles in order, summed up tile by tile: fn(b, t0, seq, extent of an item, extent
-// before the tile) for every tile, each on one thread.  Returns the total.  Called by all threads;
+// The units of all tiles in order, summed up tile by tile: fn(b, c0, seq, extent of an item,
+// extent before the tile) for every tile, each on one thread.  Returns the total.  Called by all threads;
 // s_seq, s_off: scratch for blockDim sequences.
-template <class Fn>
-__device__ __forceinline__ long long scan_tiles(const SeqAttnArgs& a, int tokens, int4* s_seq,
-                                                long long* s_warp, Fn fn) {
+template <int kChains, class Fn>
+__device__ __forceinline__ long long scan_tiles(const SeqAttnArgs& a, int4* s_seq, long long* s_warp,
+                                                Fn fn) {
   const int tid = threadIdx.x, n = blockDim.x;
   long long before = 0;
   for (int b0 = 0; b0 < a.B; b0 += n) {
     Seq s{0, 0, 0};
     if (b0 + tid < a.B) s = load_seq(a, b0 + tid);
     long long tiles;
-    const long long end = cta_scan(ceil_div(s.ql, tokens), s_warp, &tiles);
+    const long long end = cta_scan(ceil_div(count_chains(a, s.ql), kChains), s_warp, &tiles);
     s_seq[tid] = make_int4(s.q0, s.ql, s.kl, (int)end);  // .w: tiles up to this sequence's last
     __syncthreads();
     for (int w0 = 0; w0 < tiles; w0 += n) {
       const int w = w0 + tid;
-      int lo = 0, t0 = 0;
+      int lo = 0, c0 = 0;
       long long u = 0;
       if (w < tiles) {
         int hi = min(n, a.B - b0) - 1;  // the first sequence with .w > w
@@ -213,12 +226,12 @@ __device__ __forceinline__ long long scan_tiles(const SeqAttnArgs& a, int tokens
         }
         const int4 x = s_seq[lo];
         s = Seq{x.x, x.y, x.z};
-        t0 = (w - (x.w - ceil_div(x.y, tokens))) * tokens;
-        u = tile_units(t0, tokens, s, a.block) + kItemCost;
+        c0 = (w - (x.w - ceil_div(count_chains(a, s.ql), kChains))) * kChains;
+        u = tile_units<kChains>(a, c0, s) + kItemCost;
       }
       long long total;
       const long long upto = cta_scan(u * a.Hkv, s_warp, &total);
-      if (u > 0) fn(b0 + lo, t0, s, (int)u, before + upto - u * a.Hkv);
+      if (u > 0) fn(b0 + lo, c0, s, (int)u, before + upto - u * a.Hkv);
       before += total;
     }
     __syncthreads();
@@ -231,12 +244,19 @@ __device__ __forceinline__ long long snap(long long x, long long first, int n, l
   return x - first < near ? first : first + n - x < near ? first + n : x;
 }
 
-// Key tiles [j0, j0 + n) of an item that chain c takes (tpt tokens per chain).
-__device__ __forceinline__ int chain_tiles(const Item& it, int c, int tpt, int block) {
-  const int first = it.t0 + c * tpt, last = min(first + tpt, it.ql) - 1;
-  if (last < first) return 0;
-  const Seq s{it.q0, it.ql, it.kl};
-  return min(max(tiles_seen(last, s, block) - it.j0, 0), it.nk);
+// Chain c of an item: its tokens [t0, t1) (none: t0 == t1), and the key tiles [j0, j0 + n) it takes.
+struct Chain {
+  int t0, t1, n;
+};
+__device__ __forceinline__ Chain chain_of(const SeqAttnArgs& a, const Item& it, int c) {
+  Chain x{0, 0, 0};
+  if (it.c0 + c < count_chains(a, it.ql)) {
+    x.t0 = chain_start(a, it.c0 + c);
+    x.t1 = chain_end(a, it.c0 + c, it.ql);
+    const Seq s{it.q0, it.ql, it.kl};
+    x.n = min(max(tiles_seen(x.t1 - 1, s, a.block) - it.j0, 0), it.nk);
+  }
+  return x;
 }
 
 template <bool F16>
@@ -246,26 +266,54 @@ __host__ __device__ constexpr uint32_t idesc_16bit(int M, int N, int b_mn) {
          ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
+// Barriers of a chain's four softmax warps; chain_any: whether v holds on any of their threads.
+__device__ __forceinline__ void chain_barrier(int c) {
+  asm volatile("bar.sync %0, 128;" ::"r"(c + 1) : "memory");
+}
+__device__ __forceinline__ bool chain_any(int c, bool v) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "bar.red.or.pred q, %2, 128, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"((uint32_t)v), "r"(c + 1)
+      : "memory");
+  return r != 0;
+}
+
 // Replaces what is not finite in the 64 V rows of a tile by 0 (the chain's 128 threads, 16 bytes
-// each in turn); sets *flag if a row below n_valid held any.
+// each in turn).  flags[0]: there was something to replace; flags[1]: in a row below n_valid.
 template <int D, bool F16>
-__device__ __forceinline__ void scrub_v(uint16_t* v, int n_valid, int tid, volatile int* flag) {
+__device__ __forceinline__ void scrub_v(uint16_t* v, int n_valid, int tid, volatile int* flags) {
+  constexpr int kVecs = kBN * D / 8 / 128;
   uint4* p = reinterpret_cast<uint4*>(v);
+  uint4 x[kVecs];
+  bool bad = false;
 #pragma unroll
-  for (int i = 0; i < kBN * D / 8 / 128; ++i) {
-    const int e = tid + 128 * i;
-    uint4 x = p[e];
-    if (nonfinite2<F16>(x.x) || nonfinite2<F16>(x.y) || nonfinite2<F16>(x.z) || nonfinite2<F16>(x.w)) {
-      if (((e >> 3) & (kBN - 1)) < n_valid) *flag = 1;  // rows of 8 vectors, kBN rows a half
+  for (int i = 0; i < kVecs; ++i) {
+    x[i] = p[tid + 128 * i];
+    bad |= nonfinite2<F16>(x[i].x) || nonfinite2<F16>(x[i].y) || nonfinite2<F16>(x[i].z) ||
+           nonfinite2<F16>(x[i].w);
+  }
+  if (bad) {
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int e = tid + 128 * i;
+      if (!(nonfinite2<F16>(x[i].x) || nonfinite2<F16>(x[i].y) || nonfinite2<F16>(x[i].z) ||
+            nonfinite2<F16>(x[i].w)))
+        continue;
+      flags[0] = 1;
+      if (((e >> 3) & (kBN - 1)) < n_valid) flags[1] = 1;  // rows of 8 vectors, kBN rows a half
       __threadfence_block();
-      x.x = finite2<F16>(x.x);
-      x.y = finite2<F16>(x.y);
-      x.z = finite2<F16>(x.z);
-      x.w = finite2<F16>(x.w);
-      p[e] = x;
+      p[e] = make_uint4(finite2<F16>(x[i].x), finite2<F16>(x[i].y), finite2<F16>(x[i].z),
+                        finite2<F16>(x[i].w));
     }
   }
-  fence_proxy_async_smem();
+  // Zeros written here, or by another chain's threads and read here: before this chain's MMA.
+  __threadfence_block();
+  if (flags[0]) fence_proxy_async_smem();
 }
 
 // o[0 .. 32) += the values that are not finite among channels [c0, c0 + 32) of the keys [j0, j1).
@@ -293,30 +341,31 @@ __device__ __forceinline__ void add_nonfinite(const SeqAttnArgs& a, int b, int q
 
 // This CTA's run, into *run (visible after the next barrier), and its entry of the list of cut
 // items: an item whose first part is this run's end.
-__device__ __forceinline__ void find_run(const SeqAttnArgs& a, const SeqScratch& sc, int tokens,
-                                         int4* s_seq, Run* run) {
+template <int kChains>
+__device__ __forceinline__ void find_run(const SeqAttnArgs& a, const SeqScratch& sc, int4* s_seq,
+                                         Run* run) {
   __shared__ long long s_warp[32], s_begin, s_end, s_first;
   __shared__ int4 s_rec[2];
   const int P = gridDim.x, cta = blockIdx.x;
   if (threadIdx.x == 0) {
     s_rec[0] = make_int4(0, 0, 0, 0);
   }
-  const long long total = scan_tiles(a, tokens, s_seq, s_warp, [](int, int, const Seq&, int, long long) {});
+  const long long total = scan_tiles<kChains>(a, s_seq, s_warp, [](int, int, const Seq&, int, long long) {});
   const long long per = (total + P - 1) / P, near = max(per / 16, kItemCost + 4ll);
   const long long x0 = cta * per, x1 = x0 + per;
   if (threadIdx.x == 0) {
     s_begin = min(x0, total);
     s_end = min(x1, total);
-    run->b = run->t0 = run->h = run->j0 = 0;
+    run->b = run->c0 = run->h = run->j0 = 0;
   }
-  scan_tiles(a, tokens, s_seq, s_warp, [&](int b, int t0, const Seq& s, int n, long long before) {
+  scan_tiles<kChains>(a, s_seq, s_warp, [&](int b, int c0, const Seq& s, int n, long long before) {
     const long long end = before + (long long)n * a.Hkv;
     if (before <= x0 && x0 < end) {
       const int h = (int)((x0 - before) / n);
       const long long first = before + (long long)h * n, x = snap(x0, first, n, near);
       s_begin = x;
       run->b = b;
-      run->t0 = t0;
+      run->c0 = c0;
       run->h = h;
       run->j0 = x == first ? 0 : (int)(x - first) - kItemCost;  // all: from the next item on
     }
@@ -327,7 +376,7 @@ __device__ __forceinline__ void find_run(const SeqAttnArgs& a, const SeqScratch&
       if (x > first && x < first + n && x0 - first < near) {
         // The cuts k per of this item that stay: first + near <= k per <= first + n - near.
         const int last = (int)((first + n - near) / per);
-        s_rec[0] = make_int4(last - cta + 1, h, t0, b);
+        s_rec[0] = make_int4(last - cta + 1, h, c0, b);
         s_rec[1] = make_int4(s.q0, s.ql, s.kl, 0);
         s_first = first;
       }
@@ -346,9 +395,11 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
     seq_tile_kernel(const __grid_constant__ CUtensorMap tmap_q,
                     const __grid_constant__ CUtensorMap tmap_k,
                     const __grid_constant__ CUtensorMap tmap_v,
+                    const __grid_constant__ CUtensorMap tmap_out,
                     const __grid_constant__ SeqAttnArgs prm, const SeqScratch sc) {
   using C = Cfg<D>;
   constexpr int kChains = C::kChains, kStages = C::kStages, kHalves = C::kHalves;
+  constexpr uint32_t kQBufs = C::kQBufs;
   extern __shared__ unsigned char smem_raw[];
   TileSmem<D>& sm = *reinterpret_cast<TileSmem<D>*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -357,13 +408,13 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
   volatile int* abort_flag = &sm.abort_flag;
   unsigned int* err = prm.err;
   pdl_launch_dependents();
-  find_run(prm, sc, kChains * (kBM / prm.group), reinterpret_cast<int4*>(sm.q), &sm.run);
+  find_run<kChains>(prm, sc, reinterpret_cast<int4*>(sm.q), &sm.run);
   fence_proxy_async_smem();  // sm.q was scratch: before the copies into it
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < C::kQBufs; ++s) {
       mbar_init(&sm.q_full[s], 1);
-      mbar_init(&sm.q_empty[s], 5 * kChains);  // each chain's MMA warp and softmax warps
+      mbar_init(&sm.q_empty[s], 2 * kChains);  // every chain's last scores and epilogue
     }
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&sm.k_full[s], 1);
@@ -379,12 +430,13 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       mbar_init(&sm.drain[c], 1);
     }
     sm.abort_flag = 0;
-    sm.nonfinite = 0;
+    sm.nonfinite[0] = sm.nonfinite[1] = 0;
     fence_mbarrier_init();
     fence_proxy_async_smem();
     tma_prefetch_desc(&tmap_q);
     tma_prefetch_desc(&tmap_k);
     tma_prefetch_desc(&tmap_v);
+    tma_prefetch_desc(&tmap_out);
   }
   if (warp == 1) {
     tmem_alloc(&sm.tmem_base, 512);
@@ -395,9 +447,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, sm.tmem_base, 0);
 
-  const int Hkv = prm.Hkv, group = prm.group, block = prm.block;
-  const int tpt = kBM / group;  // tokens of a chain
-  const int tokens = kChains * tpt;
+  const int group = prm.group, block = prm.block, tpt = prm.chain_tokens;
 
   if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kCtrlRegs));
   if (warp == 0) {
@@ -407,11 +457,11 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
     const int log2p = prm.kv.log2_page, ps = prm.kv.page_size;
     const int ppt = kPaged ? (ps >= kBN ? 1 : kBN / ps) : 1;  // pages (boxes) of a tile
     const uint32_t box_bytes = (kPaged && ps < kBN ? ps : kBN) * 128;
-    Walk walk;
-    for (walk.start(prm, sm.run, tokens);; walk.next(prm, tokens), ++ic) {
+    Walk<kChains> walk;
+    for (walk.start(prm, sm.run);; walk.next(prm), ++ic) {
       const Item& it = walk.it;
-      const int qb = ic & 1;
-      ok = mbar_wait_warp(&sm.q_empty[qb], ((ic >> 1) & 1) ^ 1, err, abort_flag);
+      const int qb = ic % kQBufs;
+      ok = mbar_wait_warp(&sm.q_empty[qb], ((ic / kQBufs) & 1) ^ 1, err, abort_flag);
       if (!ok) break;
       if (walk.left <= 0) {  // the end of the run
         if (lane == 0) {
@@ -420,7 +470,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
         }
         break;
       }
-      const int chains = min(kChains, ceil_div(it.ql - it.t0, tpt));
+      const int chains = min(kChains, walk.n_chains - it.c0);
       if (elect_one()) {
         sm.item[ic % kItemRing] = it;
         mbar_arrive_expect_tx(&sm.q_full[qb], chains * kHalves * tpt * group * 128);
@@ -428,7 +478,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
 #pragma unroll
           for (int hf = 0; hf < kHalves; ++hf)
             tma_load_4d(sm.q[qb][c][hf], &tmap_q, &sm.q_full[qb], hf * 64, 0, it.h,
-                        it.q0 + it.t0 + c * tpt);
+                        it.q0 + chain_start(prm, it.c0 + c));
       }
       __syncwarp();
       // Page ids: lane l holds that of page first + l; `next` the 32 after them.
@@ -476,8 +526,8 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
     }
     if (!ok && lane == 0) {
       // Let the copies this warp issued land before the CTA releases its shared memory.
-      for (uint32_t i = ic > 2 ? ic - 2 : 0; i <= ic; ++i)
-        for (int t = 0; t < 1000000 && !mbar_try_wait(&sm.q_full[i & 1], (i >> 1) & 1); ++t) {}
+      for (uint32_t i = ic > kQBufs ? ic - kQBufs : 0; i <= ic; ++i)
+        for (int t = 0; t < 1000000 && !mbar_try_wait(&sm.q_full[i % kQBufs], (i / kQBufs) & 1); ++t) {}
       for (int s = 0; s < kStages; ++s) {
         if (lc > (uint32_t)s) {
           const uint32_t last = (lc - 1 - s) / kStages * kStages + s;  // last use of stage s
@@ -498,11 +548,11 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
     uint32_t lc = 0, ic = 0, g = 0, oc = 0;  // ring tiles, items, this chain's tiles, its items
     bool ok = true;
     for (;; ++ic) {
-      const int qb = ic & 1;
-      ok = mbar_wait_warp(&sm.q_full[qb], (ic >> 1) & 1, err, abort_flag);
+      const int qb = ic % kQBufs;
+      ok = mbar_wait_warp(&sm.q_full[qb], (ic / kQBufs) & 1, err, abort_flag);
       if (!ok) break;
       const Item& it = sm.item[ic % kItemRing];
-      const int nk = it.nk, n = nk < 0 ? 0 : chain_tiles(it, c, tpt, block);
+      const int nk = it.nk, n = nk < 0 ? 0 : chain_of(prm, it, c).n;
       if (nk < 0) break;
       const uint64_t dq = sdesc_sw128(smem_u32(sm.q[qb][c][0]));
       tc_fence_after();
@@ -591,18 +641,17 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
     uint32_t g = 0, lc = 0;
     bool ok = true;
     for (uint32_t ic = 0;; ++ic) {
-      ok = mbar_wait_warp(&sm.q_full[ic & 1], (ic >> 1) & 1, err, abort_flag);
-      if (!ok) break;
+      ok = mbar_wait_warp(&sm.q_full[ic % kQBufs], (ic / kQBufs) & 1, err, abort_flag);
+      // A warp that gives up takes its chain along: all four meet here and at the item's end.
+      if (chain_any(c, !ok)) break;
       const Item& it = sm.item[ic % kItemRing];
       if (it.nk < 0) break;
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sm.q_empty[ic & 1]);  // seen: its q_full may move on
-      const int n = chain_tiles(it, c, tpt, block);
-      const int tok = it.t0 + c * tpt + row_tok;  // this thread's token in its sequence
-      const bool valid = row_tok < tpt && tok < it.ql;
+      const Chain ch = chain_of(prm, it, c);
+      const int n = ch.n, tok = ch.t0 + row_tok;  // this thread's token in its sequence
+      const bool valid = row_tok < tpt && tok < ch.t1;
       const int lim = valid ? row_limit(tok, it.ql, it.kl, block) : 0;
-      // Tiles from here on hide something from some row of the item (any chain).
-      const int masked_from = max(row_limit(it.t0, it.ql, it.kl, block), 0) / kBN;
+      // Tiles from here on hide something from some row of the chain (its first, at least).
+      const int masked_from = max(row_limit(ch.t0, it.ql, it.kl, block), 0) / kBN;
       const bool active = __any_sync(0xffffffffu, valid);
       float m = kUnset, lsum = 0.f;
       // One key tile; kMasked: some row of the item does not see all of it (uniform over the
@@ -615,7 +664,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
           const int st = l % kStages;
           if (!mbar_wait_warp(&sm.v_full[st], (l / kStages) & 1, err, abort_flag)) return false;
           if (it.j0 + jj >= masked_from)
-            scrub_v<D, F16>(sm.v[st][0], it.kl - (it.j0 + jj) * kBN, row, &sm.nonfinite);
+            scrub_v<D, F16>(sm.v[st][0], it.kl - (it.j0 + jj) * kBN, row, sm.nonfinite);
         }
         tc_fence_after();
         float s[kBN], pmx[kBN / 32];
@@ -625,8 +674,8 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
         tc_fence_before();
         mbar_arrive(&sm.s_empty[c]);  // the MMA warp may overwrite S_c now
         float mx = fmaxf(pmx[0], pmx[1]);
-        if (kMasked) {
-          const int n_seen = lim - (it.j0 + jj) * kBN;
+        const int n_seen = valid ? lim - (it.j0 + jj) * kBN : kBN;
+        if (kMasked && __any_sync(0xffffffffu, flip || n_seen < kBN)) {
 #pragma unroll
           for (int i = 0; i < kBN; ++i) {
             if (flip) s[i] = -s[i];
@@ -705,7 +754,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
           ok = mbar_wait_warp(&sm.s_full[c], g & 1, err, abort_flag);
           if (ok && j >= masked_from) {
             ok = mbar_wait_warp(&sm.v_full[st], (l / kStages) & 1, err, abort_flag);
-            if (ok) scrub_v<D, F16>(sm.v[st][0], it.kl - j * kBN, row, &sm.nonfinite);
+            if (ok) scrub_v<D, F16>(sm.v[st][0], it.kl - j * kBN, row, sm.nonfinite);
           }
           if (!ok) break;
           mbar_arrive(&sm.s_empty[c]);
@@ -713,71 +762,77 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
           if (ok) mbar_arrive(&sm.p_full[c]);
         }
       }
-      if (!ok) break;
       lc += it.nk;
-      if (n > 0) {
-        ok = mbar_wait_warp(&sm.o_bar[c], (g - 1) & 1, err, abort_flag);
-        if (!ok) break;
-        tc_fence_after();
-        __threadfence_block();
-      }
-      const bool refill = n > 0 && *(volatile int*)&sm.nonfinite != 0;
-      const int head = it.h * group + row_head;
-      if (it.nk < it.all) {  // a part: unnormalised O, m and l
-        const size_t r = ((size_t)(2 * cta + (it.part > 0)) * kChains + c) * kBM + row;
+      if (n > 0 && ok) ok = mbar_wait_warp(&sm.o_bar[c], (g - 1) & 1, err, abort_flag);
+      if (chain_any(c, !ok)) break;
+      tc_fence_after();
+      // Where chains may have taken values out of V: from the item's first hidden key on.
+      const int refill_from =
+          max(it.j0, max(row_limit(chain_start(prm, it.c0), it.ql, it.kl, block), 0) / kBN) * kBN;
+      const bool refill = n > 0 && *(volatile int*)&sm.nonfinite[1] != 0;
+      const bool part = it.nk < it.all;
+      // The chain's rows go out through its Q tile (no longer needed: o_bar follows the last scores)
+      // in one copy, unless the next sequence's rows would be among them.
+      const bool staged = !part && ch.t1 - ch.t0 == tpt;
+      const float inv = part ? 1.f : 1.f / lsum;
+      uint16_t* stage = sm.q[ic % kQBufs][c][0];
 #pragma unroll
-        for (int q = 0; q < D / 32; ++q) {
-          if (n == 0) break;
-          float o[32];
+      for (int q = 0; q < D / 32; ++q) {
+        float o[32];
+        if (n > 0) {
           tmem_ld32(t_o + 32 * q, o);
           tmem_wait_ld();
           if (q == D / 32 - 1) {
             tc_fence_before();
             mbar_arrive(&sm.o_empty[c]);
           }
-          if (!valid) continue;
-          if (refill)
-            add_nonfinite<D, F16, kPaged>(prm, it.b, it.q0, it.h, 32 * q, max(it.j0, masked_from) * kBN,
-                                          min(lim, (it.j0 + n) * kBN), o);
-          float4* dst = reinterpret_cast<float4*>(sc.part_o + r * D + 32 * q);
+        }
+        if (!valid) continue;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) o[i] = lim > 0 && n > 0 ? o[i] * inv : 0.f;
+        if (refill)
+          add_nonfinite<D, F16, kPaged>(prm, it.b, it.q0, it.h, 32 * q, refill_from,
+                                        min(lim, (it.j0 + n) * kBN), o);
+        if (part) {  // [slot][chain][D / 4][128 rows] of four channels
+          float4* dst = reinterpret_cast<float4*>(sc.part_o) +
+                        ((size_t)((2 * cta + (it.part > 0)) * kChains + c) * (D / 4) + 8 * q) * kBM + row;
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-        }
-        if (valid) sc.part_ml[r] = make_float2(m, lsum);
-      } else {
-        const float inv = 1.f / lsum;
-        uint16_t* out = prm.out + (int64_t)(it.q0 + tok) * prm.out_stride + head * D;
-#pragma unroll
-        for (int q = 0; q < D / 32; ++q) {
-          float o[32];
-          if (n > 0) {
-            tmem_ld32(t_o + 32 * q, o);
-            tmem_wait_ld();
-            if (q == D / 32 - 1) {
-              tc_fence_before();
-              mbar_arrive(&sm.o_empty[c]);
-            }
-          }
-          if (!valid) continue;
-#pragma unroll
-          for (int i = 0; i < 32; ++i) o[i] = lim > 0 ? o[i] * inv : 0.f;
-          if (refill)
-            add_nonfinite<D, F16, kPaged>(prm, it.b, it.q0, it.h, 32 * q, max(it.j0, masked_from) * kBN,
-                                          min(lim, (it.j0 + n) * kBN), o);
-          uint4* dst = reinterpret_cast<uint4*>(out + 32 * q);
+            dst[i * kBM] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        } else {
+          uint16_t* to = staged ? stage + (q >> 1) * (kBM * 64) + row * 64
+                                : prm.out + (int64_t)(it.q0 + tok) * prm.out_stride +
+                                      (it.h * group + row_head) * D + (q >> 1) * 64;
+          const int swizzle = staged ? row & 7 : 0;
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            dst[i] = make_uint4(pack2<F16>(o[8 * i], o[8 * i + 1]), pack2<F16>(o[8 * i + 2], o[8 * i + 3]),
-                                pack2<F16>(o[8 * i + 4], o[8 * i + 5]),
-                                pack2<F16>(o[8 * i + 6], o[8 * i + 7]));
+            *reinterpret_cast<uint4*>(to + ((4 * (q & 1) + i) ^ swizzle) * 8) =
+                make_uint4(pack2<F16>(o[8 * i], o[8 * i + 1]), pack2<F16>(o[8 * i + 2], o[8 * i + 3]),
+                           pack2<F16>(o[8 * i + 4], o[8 * i + 5]), pack2<F16>(o[8 * i + 6], o[8 * i + 7]));
         }
-        if (valid && prm.lse)
-          prm.lse[(size_t)(it.q0 + tok) * prm.Hq + head] =
-              lim > 0 ? (m + log2f(lsum)) * 0.69314718055994531f : -INFINITY;
+      }
+      if (part) {
+        if (valid)
+          sc.part_ml[((size_t)(2 * cta + (it.part > 0)) * kChains + c) * kBM + row] = make_float2(m, lsum);
+      } else if (valid && prm.lse) {
+        prm.lse[(size_t)(it.q0 + tok) * prm.Hq + it.h * group + row_head] =
+            lim > 0 ? (m + log2f(lsum)) * 0.69314718055994531f : -INFINITY;
+      }
+      fence_proxy_async_smem();
+      chain_barrier(c);
+      if (quarter == 0 && lane == 0) {
+        if (staged) {
+#pragma unroll
+          for (int hf = 0; hf < kHalves; ++hf)
+            tma_store_4d(&tmap_out, stage + hf * (kBM * 64), hf * 64, 0, it.h, it.q0 + ch.t0);
+          tma_store_commit();
+          tma_store_wait_read<0>();
+        }
+        mbar_arrive(&sm.q_empty[ic % kQBufs]);
       }
       __syncwarp();
     }
+    if (quarter == 0 && lane == 0) tma_store_wait_all();
   }
 
   tc_fence_before();
@@ -805,13 +860,15 @@ ScratchLayout scratch_layout(int d) {
 template <int D, bool F16, bool kPaged>
 cudaError_t launch_tiles(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms, cudaStream_t st) {
   using C = Cfg<D>;
-  CUtensorMap mq, mk, mv;
+  CUtensorMap mq, mk, mv, mo;
   const uint64_t g = a.group, H = a.Hkv;
-  const int tpt = kBM / a.group;
   const uint64_t qd[4] = {D, g, H, (uint64_t)a.T};
   const uint64_t qs[3] = {D, g * D, (uint64_t)a.q_stride};
-  const uint32_t qb[4] = {64, (uint32_t)g, 1, (uint32_t)tpt};
+  const uint32_t qb[4] = {64, (uint32_t)g, 1, (uint32_t)a.chain_tokens};
   cudaError_t e = make_tmap_16bit_4d(&mq, a.q, F16, qd, qs, qb);
+  if (e != cudaSuccess) return e;
+  const uint64_t os[3] = {D, g * D, (uint64_t)a.out_stride};
+  e = make_tmap_16bit_4d(&mo, a.out, F16, qd, os, qb);
   if (e != cudaSuccess) return e;
   e = make_kv_maps(a, kBN, &mk, &mv);
   if (e != cudaSuccess) return e;
@@ -820,7 +877,7 @@ cudaError_t launch_tiles(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms
   const void* tile = reinterpret_cast<const void*>(seq_tile_kernel<D, F16, kPaged>);
   e = cudaFuncSetAttribute(tile, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  seq_tile_kernel<D, F16, kPaged><<<P, C::kThreads, smem, st>>>(mq, mk, mv, a, sc);
+  seq_tile_kernel<D, F16, kPaged><<<P, C::kThreads, smem, st>>>(mq, mk, mv, mo, a, sc);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   return launch_seq_join(a, sc, true, P, st);

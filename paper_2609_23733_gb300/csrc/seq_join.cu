@@ -30,18 +30,21 @@ __global__ void __launch_bounds__(kThreads)
   const int4 x = sc.recs[2 * cta], y = sc.recs[2 * cta + 1];
   const int np = x.x;
   if (np == 0) return;
-  const int tid = threadIdx.x, c = (tid % kLanes) * 4, sub = tid / kLanes % kSub;
-  const int tpt = 128 / a.group;
+  // Threads of a row: kSub groups of D / 4.  The tile kernel's parts have a row's neighbours side by
+  // side, the other's its channels.
+  const int tid = threadIdx.x;
+  const int c = (kTiles ? tid / kRowsCta : tid % kLanes) * 4, sub = kTiles ? 0 : tid / kLanes % kSub;
   auto slot = [&](int i) { return (size_t)(i == 0 ? y.w : 2 * (cta + i)); };
   for (int base = blockIdx.y * kRowsCta; base < kRows; base += gridDim.y * kRowsCta) {
-    const int r = base + tid / (kLanes * kSub);
+    const int r = base + (kTiles ? tid % kRowsCta : tid / (kLanes * kSub));
     int tok, sub_head;
     bool valid;
     if (kTiles) {  // chain, row of the chain
-      const int row = r % 128, t = row / a.group;
-      tok = x.z + (r / 128) * tpt + t;
+      const int chain = x.z + r / 128, row = r % 128, t = row / a.group;
+      valid = chain < count_chains(a, y.y) && t < a.chain_tokens;
+      tok = (valid ? chain_start(a, chain) : 0) + t;
       sub_head = row - t * a.group;
-      valid = t < tpt && tok < y.y;
+      valid = valid && tok < chain_end(a, chain, y.y);
     } else {
       const int row = x.z * kSmallRows + r;
       tok = row / a.group;
@@ -55,7 +58,9 @@ __global__ void __launch_bounds__(kThreads)
       for (int i = sub; i < np; i += kSub) {
         const size_t row = slot(i) * kRows + r;
         const float2 ml = sc.part_ml[row];
-        const float4 v = *reinterpret_cast<const float4*>(sc.part_o + row * D + c);
+        const float4 v = *reinterpret_cast<const float4*>(
+            sc.part_o + (kTiles ? ((slot(i) * (kRows / 128) + r / 128) * (D / 4) + c / 4) * 512 + (r % 128) * 4
+                                : row * D + c));
         const float f = fast_exp2(ml.x - m);
         if (ml.y != 0.f) {  // else nothing was visible there, and O may be unwritten
           l = fmaf(f, ml.y, l);
