@@ -138,7 +138,7 @@ __device__ __forceinline__ int row_limit(int i, int ql, int kl, int block) {
 // do not run across mask blocks, so that all rows of a chain see the same keys.
 __device__ __forceinline__ int count_chains(const SeqAttnArgs& a, int ql) {
   const int n = a.chain_tokens;
-  if (a.block_chains == 0) return (int)(((long long)ql + n - 1) / n);
+  if (a.block_chains == 0) return (ql + n - 1) / n;  // ql <= 2^30
   const int full = ql / a.block;
   return full * a.block_chains + (ql - full * a.block + n - 1) / n;
 }

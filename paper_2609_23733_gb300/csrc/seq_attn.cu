@@ -63,10 +63,7 @@ __device__ __forceinline__ int tile_units(const SeqAttnArgs& a, int c0, const Se
 // An item costs about as much as this many units on top of its own (its Q, first scores and
 // epilogue, which the other chains hide only in part).
 #ifndef VP_SEQ_ITEM_COST
-#define VP_SEQ_ITEM_COST 8
-#endif
-#ifndef VP_Q128
-#define VP_Q128 2
+#define VP_SEQ_ITEM_COST 5
 #endif
 constexpr int kItemCost = VP_SEQ_ITEM_COST;
 
@@ -81,6 +78,23 @@ struct Run {
 struct Item {
   int b, c0, h, j0, nk, all, q0, ql, kl, part;
 };
+// Chain c of an item: its tokens [t0, t1) (none: t0 == t1), the key tiles [j0, j0 + n) it takes,
+// and the tile from which on something is hidden from some row of it (its first, at least).
+struct Chain {
+  int t0, t1, n, masked_from;
+};
+__device__ __forceinline__ Chain chain_of(const SeqAttnArgs& a, const Item& it, int c, int n_chains) {
+  Chain x{0, 0, 0, 0};
+  if (it.c0 + c < n_chains) {
+    x.t0 = chain_start(a, it.c0 + c);
+    x.t1 = chain_end(a, it.c0 + c, it.ql);
+    const Seq s{it.q0, it.ql, it.kl};
+    x.n = min(max(tiles_seen(x.t1 - 1, s, a.block) - it.j0, 0), it.nk);
+    x.masked_from = max(row_limit(x.t0, s.ql, s.kl, a.block), 0) / kBN;
+  }
+  return x;
+}
+
 // Items in flight between the producer and the epilogues: with two Q buffers, the producer writes
 // item i + 2 after item i's epilogue.
 constexpr int kItemRing = 4;
@@ -148,8 +162,8 @@ template <int D>
 struct Cfg {
   static constexpr int kChains = seq_chains(D);
   static constexpr int kHalves = D / 64;               // 64-channel (128-byte) column blocks
-  static constexpr int kQBufs = D == 64 ? 2 : VP_Q128;
-  static constexpr int kStages = D == 64 ? 8 : (VP_Q128 == 2 ? 3 : 5);      // of 64 keys: 128 / 96 KB of K and V
+  static constexpr int kQBufs = 2;
+  static constexpr int kStages = D == 64 ? 8 : 3;      // of 64 keys: 128 / 96 KB of K and V
   static constexpr int kThreads = 128 + 128 * kChains;
   static constexpr int kCtrlRegs = kChains == 3 ? 56 : 80;
   static constexpr int kSoftRegs = kChains == 3 ? 152 : 208;
@@ -173,7 +187,8 @@ struct TileSmem {
   int abort_flag;
   int nonfinite[2];  // V values of masked tiles replaced by 0: any, and any that some row sees
   Run run;
-  Item item[kItemRing];  // published by the producer with q_full
+  Item item[kItemRing];  // published by the producer with q_full, and their chains
+  Chain chain[kItemRing][C::kChains];
 };
 
 // Inclusive scan of v over the CTA's threads; *total: the sum.  s_warp: one value per warp.
@@ -244,21 +259,6 @@ __device__ __forceinline__ long long snap(long long x, long long first, int n, l
   return x - first < near ? first : first + n - x < near ? first + n : x;
 }
 
-// Chain c of an item: its tokens [t0, t1) (none: t0 == t1), and the key tiles [j0, j0 + n) it takes.
-struct Chain {
-  int t0, t1, n;
-};
-__device__ __forceinline__ Chain chain_of(const SeqAttnArgs& a, const Item& it, int c) {
-  Chain x{0, 0, 0};
-  if (it.c0 + c < count_chains(a, it.ql)) {
-    x.t0 = chain_start(a, it.c0 + c);
-    x.t1 = chain_end(a, it.c0 + c, it.ql);
-    const Seq s{it.q0, it.ql, it.kl};
-    x.n = min(max(tiles_seen(x.t1 - 1, s, a.block) - it.j0, 0), it.nk);
-  }
-  return x;
-}
-
 template <bool F16>
 __host__ __device__ constexpr uint32_t idesc_16bit(int M, int N, int b_mn) {
   // D fp32; A and B bf16 (1) or fp16 (0); A K-major, B K-major or MN-major
@@ -316,27 +316,42 @@ __device__ __forceinline__ void scrub_v(uint16_t* v, int n_valid, int tid, volat
   if (flags[0]) fence_proxy_async_smem();
 }
 
-// o[0 .. 32) += the values that are not finite among channels [c0, c0 + 32) of the keys [j0, j1).
-template <int D, bool F16, bool kPaged>
-__device__ __forceinline__ void add_nonfinite(const SeqAttnArgs& a, int b, int q0, int h, int c0,
-                                              int j0, int j1, float (&o)[32]) {
+// Adds to a row of outputs in memory the V values that are not finite among the keys [j0, j1).
+// at(c): reads channel c; put(c, x): writes it.
+template <int D, bool F16, bool kPaged, class At, class Put>
+__device__ __forceinline__ void add_nonfinite(const SeqAttnArgs& a, const Item& it, int j0, int j1, At at,
+                                              Put put) {
 #pragma unroll 1
   for (int j = j0; j < j1; ++j) {
     const uint16_t* row;
     if constexpr (kPaged) {
-      const int page = a.kv.table[(size_t)b * a.kv.width + (j >> a.kv.log2_page)];
+      const int page = a.kv.table[(size_t)it.b * a.kv.width + (j >> a.kv.log2_page)];
       if ((unsigned)page >= (unsigned)a.kv.n_pages) continue;
-      row = a.kv.v + (((((long long)page * a.Hkv + h) << a.kv.log2_page)) + (j & (a.kv.page_size - 1))) * D;
+      row = a.kv.v +
+            (((((long long)page * a.Hkv + it.h) << a.kv.log2_page)) + (j & (a.kv.page_size - 1))) * D;
     } else {
-      row = a.v + (long long)(q0 + j) * a.v_stride + h * D;
+      row = a.v + (long long)(it.q0 + j) * a.v_stride + it.h * D;
     }
-#pragma unroll
-    for (int c = 0; c < 32; c += 2) {
-      const float2 x = unpack2<F16>(*reinterpret_cast<const uint32_t*>(row + c0 + c));
-      if (!isfinite(x.x)) o[c] += x.x;
-      if (!isfinite(x.y)) o[c + 1] += x.y;
+#pragma unroll 1
+    for (int c = 0; c < D; ++c) {
+      const float x = to_float<F16>(row[c]);
+      if (!isfinite(x)) put(c, at(c) + x);
     }
   }
+}
+template <int D, bool F16, bool kPaged>
+__device__ __noinline__ void refill_out(const SeqAttnArgs& a, const Item& it, int j0, int j1, uint16_t* out,
+                                        int half_pitch, int swizzle) {
+  auto addr = [&](int c) { return out + (c >> 6) * half_pitch + ((((c & 63) >> 3) ^ swizzle) << 3) + (c & 7); };
+  add_nonfinite<D, F16, kPaged>(
+      a, it, j0, j1, [&](int c) { return to_float<F16>(*addr(c)); },
+      [&](int c, float x) { *addr(c) = (uint16_t)pack2<F16>(x, 0.f); });
+}
+template <int D, bool F16, bool kPaged>
+__device__ __noinline__ void refill_part(const SeqAttnArgs& a, const Item& it, int j0, int j1, float* part) {
+  auto addr = [&](int c) { return part + (c >> 2) * (4 * kBM) + (c & 3); };
+  add_nonfinite<D, F16, kPaged>(
+      a, it, j0, j1, [&](int c) { return *addr(c); }, [&](int c, float x) { *addr(c) = x; });
 }
 
 // This CTA's run, into *run (visible after the next barrier), and its entry of the list of cut
@@ -471,8 +486,10 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
         break;
       }
       const int chains = min(kChains, walk.n_chains - it.c0);
+      if (lane == 0) sm.item[ic % kItemRing] = it;
+      if (lane < kChains) sm.chain[ic % kItemRing][lane] = chain_of(prm, it, lane, walk.n_chains);
+      __syncwarp();
       if (elect_one()) {
-        sm.item[ic % kItemRing] = it;
         mbar_arrive_expect_tx(&sm.q_full[qb], chains * kHalves * tpt * group * 128);
         for (int c = 0; c < chains; ++c)
 #pragma unroll
@@ -552,7 +569,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       ok = mbar_wait_warp(&sm.q_full[qb], (ic / kQBufs) & 1, err, abort_flag);
       if (!ok) break;
       const Item& it = sm.item[ic % kItemRing];
-      const int nk = it.nk, n = nk < 0 ? 0 : chain_of(prm, it, c).n;
+      const int nk = it.nk, n = sm.chain[ic % kItemRing][c].n;
       if (nk < 0) break;
       const uint64_t dq = sdesc_sw128(smem_u32(sm.q[qb][c][0]));
       tc_fence_after();
@@ -639,6 +656,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
     const bool flip = prm.scale_log2 < 0.f;  // scores are negated, so that the maximum is the scores'
     const float cs = fmaxf(fabsf(prm.scale_log2), 1e-30f);
     uint32_t g = 0, lc = 0;
+    int owed = -1;  // item whose Q tile the copy of its outputs may still be reading (one thread)
     bool ok = true;
     for (uint32_t ic = 0;; ++ic) {
       ok = mbar_wait_warp(&sm.q_full[ic % kQBufs], (ic / kQBufs) & 1, err, abort_flag);
@@ -646,14 +664,21 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       if (chain_any(c, !ok)) break;
       const Item& it = sm.item[ic % kItemRing];
       if (it.nk < 0) break;
-      const Chain ch = chain_of(prm, it, c);
+      const Chain ch = sm.chain[ic % kItemRing][c];
       const int n = ch.n, tok = ch.t0 + row_tok;  // this thread's token in its sequence
       const bool valid = row_tok < tpt && tok < ch.t1;
       const int lim = valid ? row_limit(tok, it.ql, it.kl, block) : 0;
-      // Tiles from here on hide something from some row of the chain (its first, at least).
-      const int masked_from = max(row_limit(ch.t0, it.ql, it.kl, block), 0) / kBN;
+      const int masked_from = ch.masked_from;
       const bool active = __any_sync(0xffffffffu, valid);
       float m = kUnset, lsum = 0.f;
+      // The copy of the item before had this item's start to read its Q tile.
+      auto release_q = [&] {
+        if (owed >= 0) {
+          tma_store_wait_read<0>();
+          mbar_arrive(&sm.q_empty[owed % kQBufs]);
+          owed = -1;
+        }
+      };
       // One key tile; kMasked: some row of the item does not see all of it (uniform over the
       // chains), or the scores are negated.
       auto tile = [&](auto masked_const, int jj) -> bool {
@@ -738,9 +763,11 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive(&sm.p_full[c]);
+        if (jj == 0) release_q();
         ++g;
         return true;
       };
+      if (n == 0) release_q();
       if (active) {
         const int clear = flip ? 0 : min(max(masked_from - it.j0, 0), n);
         int jj = 0;
@@ -766,16 +793,18 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       if (n > 0 && ok) ok = mbar_wait_warp(&sm.o_bar[c], (g - 1) & 1, err, abort_flag);
       if (chain_any(c, !ok)) break;
       tc_fence_after();
-      // Where chains may have taken values out of V: from the item's first hidden key on.
-      const int refill_from =
-          max(it.j0, max(row_limit(chain_start(prm, it.c0), it.ql, it.kl, block), 0) / kBN) * kBN;
-      const bool refill = n > 0 && *(volatile int*)&sm.nonfinite[1] != 0;
       const bool part = it.nk < it.all;
       // The chain's rows go out through its Q tile (no longer needed: o_bar follows the last scores)
       // in one copy, unless the next sequence's rows would be among them.
       const bool staged = !part && ch.t1 - ch.t0 == tpt;
-      const float inv = part ? 1.f : 1.f / lsum;
+      const float inv = part ? 1.f : lim > 0 ? 1.f / lsum : 0.f;
       uint16_t* stage = sm.q[ic % kQBufs][c][0];
+      // Rows: of two 64-channel halves, 16-byte chunks in the swizzled order of the staged tile.
+      uint16_t* to = staged ? stage + row * 64
+                            : prm.out + (int64_t)(it.q0 + tok) * prm.out_stride + (it.h * group + row_head) * D;
+      const int half_pitch = staged ? kBM * 64 : 64, swizzle = staged ? row & 7 : 0;
+      const size_t slot_chain = (size_t)(2 * cta + (it.part > 0)) * kChains + c;
+      float* to_part = sc.part_o + (slot_chain * (D / 4) * kBM + row) * 4;  // [D / 4][128 rows][4]
 #pragma unroll
       for (int q = 0; q < D / 32; ++q) {
         float o[32];
@@ -786,39 +815,40 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
             tc_fence_before();
             mbar_arrive(&sm.o_empty[c]);
           }
-        }
-        if (!valid) continue;
-#pragma unroll
-        for (int i = 0; i < 32; ++i) o[i] = lim > 0 && n > 0 ? o[i] * inv : 0.f;
-        if (refill)
-          add_nonfinite<D, F16, kPaged>(prm, it.b, it.q0, it.h, 32 * q, refill_from,
-                                        min(lim, (it.j0 + n) * kBN), o);
-        if (part) {  // [slot][chain][D / 4][128 rows] of four channels
-          float4* dst = reinterpret_cast<float4*>(sc.part_o) +
-                        ((size_t)((2 * cta + (it.part > 0)) * kChains + c) * (D / 4) + 8 * q) * kBM + row;
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            dst[i * kBM] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
         } else {
-          uint16_t* to = staged ? stage + (q >> 1) * (kBM * 64) + row * 64
-                                : prm.out + (int64_t)(it.q0 + tok) * prm.out_stride +
-                                      (it.h * group + row_head) * D + (q >> 1) * 64;
-          const int swizzle = staged ? row & 7 : 0;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] = 0.f;
+        }
+        if (part) {
+          if (valid)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              *reinterpret_cast<float4*>(to_part + (8 * q + i) * (4 * kBM)) =
+                  make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        } else if (valid) {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<uint4*>(to + ((4 * (q & 1) + i) ^ swizzle) * 8) =
-                make_uint4(pack2<F16>(o[8 * i], o[8 * i + 1]), pack2<F16>(o[8 * i + 2], o[8 * i + 3]),
-                           pack2<F16>(o[8 * i + 4], o[8 * i + 5]), pack2<F16>(o[8 * i + 6], o[8 * i + 7]));
+            *reinterpret_cast<uint4*>(to + (q >> 1) * half_pitch + ((4 * (q & 1) + i) ^ swizzle) * 8) =
+                make_uint4(pack2<F16>(o[8 * i] * inv, o[8 * i + 1] * inv),
+                           pack2<F16>(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
+                           pack2<F16>(o[8 * i + 4] * inv, o[8 * i + 5] * inv),
+                           pack2<F16>(o[8 * i + 6] * inv, o[8 * i + 7] * inv));
         }
       }
-      if (part) {
-        if (valid)
-          sc.part_ml[((size_t)(2 * cta + (it.part > 0)) * kChains + c) * kBM + row] = make_float2(m, lsum);
-      } else if (valid && prm.lse) {
+      if (n > 0 && valid && *(volatile int*)&sm.nonfinite[1] != 0) {
+        // Chains may have taken values out of V from the item's first hidden key on.
+        const int j0 = max(it.j0, sm.chain[ic % kItemRing][0].masked_from) * kBN;
+        const int j1 = min(lim, (it.j0 + n) * kBN);
+        if (part)
+          refill_part<D, F16, kPaged>(prm, it, j0, j1, to_part);
+        else
+          refill_out<D, F16, kPaged>(prm, it, j0, j1, to, half_pitch, swizzle);
+      }
+      if (valid && part) sc.part_ml[slot_chain * kBM + row] = make_float2(m, lsum);
+      if (valid && !part && prm.lse)
         prm.lse[(size_t)(it.q0 + tok) * prm.Hq + it.h * group + row_head] =
             lim > 0 ? (m + log2f(lsum)) * 0.69314718055994531f : -INFINITY;
-      }
-      fence_proxy_async_smem();
+      if (staged) fence_proxy_async_smem();
       chain_barrier(c);
       if (quarter == 0 && lane == 0) {
         if (staged) {
@@ -826,9 +856,10 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
           for (int hf = 0; hf < kHalves; ++hf)
             tma_store_4d(&tmap_out, stage + hf * (kBM * 64), hf * 64, 0, it.h, it.q0 + ch.t0);
           tma_store_commit();
-          tma_store_wait_read<0>();
+          owed = ic;  // Q is free once the copy has read it: waited for in the next item
+        } else {
+          mbar_arrive(&sm.q_empty[ic % kQBufs]);
         }
-        mbar_arrive(&sm.q_empty[ic % kQBufs]);
       }
       __syncwarp();
     }
