@@ -39,13 +39,44 @@ namespace vp {
 namespace {
 
 constexpr int kBM = 128;   // rows of a chain
-constexpr int kBN = 64;    // keys of a tile
 constexpr float kUnset = -1e30f;           // running maximum before the first visible key
 constexpr float kRescaleThreshold = 8.f;   // log2 units
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
+#ifndef VP_SEQ_ITEM_COST
+#define VP_SEQ_ITEM_COST 5
+#endif
+#ifndef VP_SEQ_ITEM_COST128
+#define VP_SEQ_ITEM_COST128 3
+#endif
+template <int D>
+struct Cfg {
+  static constexpr int kChains = seq_chains(D);
+  static constexpr int kBN = D == 64 ? 64 : 128;       // keys of a tile
+  static constexpr bool kAlias = D == 128;             // P lies in the first columns of S
+  static constexpr int kHalves = D / 64;               // 64-channel (128-byte) column blocks
+  static constexpr int kQTiles = D == 64 ? 6 : 3;      // Q tiles of chains, in turn: 96 KB
+  static constexpr int kStages = D == 64 ? 8 : 2;      // 128 KB of K and V
+  static constexpr int kThreads = 128 + 128 * kChains;
+  static constexpr int kCtrlRegs = kChains == 3 ? 56 : 80;
+  static constexpr int kSoftRegs = kChains == 3 ? 152 : 208;
+  static_assert(128 * kCtrlRegs + 128 * kChains * kSoftRegs <= 65536, "register split");
+  // TMEM columns: S_c (fp32), O_c (fp32), P_c (16-bit pairs) of every chain.
+  static constexpr uint32_t kColS = 0, kColO = kChains * kBN, kColP = kAlias ? kColS : kColO + kChains * D;
+  static constexpr uint32_t kPitchP = kAlias ? kBN : kBN / 2;
+  static_assert((kAlias ? kColO + kChains * D : kColP + kChains * kBN / 2) <= 512, "TMEM columns");
+  // An item costs about as much as this many units on top of its own (its Q, first scores and
+  // epilogue, which the other chains hide only in part).
+  static constexpr int kItemCost = D == 64 ? VP_SEQ_ITEM_COST : VP_SEQ_ITEM_COST128;
+};
+
+// A value that is the same on all lanes, in a form that lets the compiler see it: what tcgen05 and TMA
+// instructions, and the branches around them, are given stays in uniform registers.
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+
 // Key tiles that a token sees.
+template <int kBN>
 __device__ __forceinline__ int tiles_seen(int token, const Seq& s, int block) {
   const int lim = row_limit(token, s.ql, s.kl, block);
   return lim > 0 ? ceil_div(lim, kBN) : 0;
@@ -53,20 +84,13 @@ __device__ __forceinline__ int tiles_seen(int token, const Seq& s, int block) {
 
 // Key tiles (units) of the tile that begins with chain c0, kChains at most; at least one, in which
 // rows that see nothing get their zeros.
-template <int kChains>
+template <class C>
 __device__ __forceinline__ int tile_units(const SeqAttnArgs& a, int c0, const Seq& s) {
-  const int last = min(c0 + kChains, count_chains(a, s.ql)) - 1;
-  return max(1, tiles_seen(chain_end(a, last, s.ql) - 1, s, a.block));
+  const int last = min(c0 + C::kChains, count_chains(a, s.ql)) - 1;
+  return max(1, tiles_seen<C::kBN>(chain_end(a, last, s.ql) - 1, s, a.block));
 }
 
 // ------------------------------------------------------------------ runs of units
-// An item costs about as much as this many units on top of its own (its Q, first scores and
-// epilogue, which the other chains hide only in part).
-#ifndef VP_SEQ_ITEM_COST
-#define VP_SEQ_ITEM_COST 5
-#endif
-constexpr int kItemCost = VP_SEQ_ITEM_COST;
-
 // A CTA's run: the first segment, and its extent in units, kItemCost for every item begun included.
 struct Run {
   int b, c0, h, j0;
@@ -79,18 +103,19 @@ struct Item {
   int b, c0, h, j0, nk, all, q0, ql, kl, part;
 };
 // Chain c of an item: its tokens [t0, t1) (none: t0 == t1), the key tiles [j0, j0 + n) it takes,
-// and the tile from which on something is hidden from some row of it (its first, at least).
+// and the first key that is hidden from some row of it (from its first token's).
 struct Chain {
-  int t0, t1, n, masked_from;
+  int t0, t1, n, hidden_from;
 };
+template <int kBN>
 __device__ __forceinline__ Chain chain_of(const SeqAttnArgs& a, const Item& it, int c, int n_chains) {
   Chain x{0, 0, 0, 0};
   if (it.c0 + c < n_chains) {
     x.t0 = chain_start(a, it.c0 + c);
     x.t1 = chain_end(a, it.c0 + c, it.ql);
     const Seq s{it.q0, it.ql, it.kl};
-    x.n = min(max(tiles_seen(x.t1 - 1, s, a.block) - it.j0, 0), it.nk);
-    x.masked_from = max(row_limit(x.t0, s.ql, s.kl, a.block), 0) / kBN;
+    x.n = min(max(tiles_seen<kBN>(x.t1 - 1, s, a.block) - it.j0, 0), it.nk);
+    x.hidden_from = max(row_limit(x.t0, s.ql, s.kl, a.block), 0);
   }
   return x;
 }
@@ -100,8 +125,9 @@ __device__ __forceinline__ Chain chain_of(const SeqAttnArgs& a, const Item& it, 
 constexpr int kItemRing = 4;
 
 // The segments of a run, one after another.
-template <int kChains>
+template <class C>
 struct Walk {
+  static constexpr int kChains = C::kChains, kItemCost = C::kItemCost;
   Item it;
   long long left;  // extent from this segment on
   int here;        // this segment's extent, were its item not cut
@@ -109,24 +135,24 @@ struct Walk {
 
   __device__ __forceinline__ void load(const SeqAttnArgs& a) {
     const Seq s = load_seq(a, it.b);
-    it.q0 = s.q0;
-    it.ql = s.ql;
-    it.kl = s.kl;
-    n_chains = count_chains(a, s.ql);
+    it.q0 = uniform(s.q0);
+    it.ql = uniform(s.ql);
+    it.kl = uniform(s.kl);
+    n_chains = count_chains(a, it.ql);
   }
   __device__ __forceinline__ void set(const SeqAttnArgs& a) {
-    it.all = tile_units<kChains>(a, it.c0, Seq{it.q0, it.ql, it.kl});
+    it.all = tile_units<C>(a, it.c0, Seq{it.q0, it.ql, it.kl});
     const int cost = it.j0 == 0 ? kItemCost : 0;
     here = it.all - it.j0 + cost;
     it.nk = left >= here ? it.all - it.j0 : (int)left - cost;
   }
   __device__ __forceinline__ void start(const SeqAttnArgs& a, const Run& r) {
-    it.b = r.b;
-    it.c0 = r.c0;
-    it.h = r.h;
-    it.j0 = r.j0;
+    it.b = uniform(r.b);
+    it.c0 = uniform(r.c0);
+    it.h = uniform(r.h);
+    it.j0 = uniform(r.j0);
     it.part = 0;
-    left = r.units;
+    left = __shfl_sync(0xffffffffu, r.units, 0);
     if (left > 0) {
       load(a);
       set(a);
@@ -159,30 +185,16 @@ struct Walk {
 
 // ------------------------------------------------------------------ tile kernel
 template <int D>
-struct Cfg {
-  static constexpr int kChains = seq_chains(D);
-  static constexpr int kHalves = D / 64;               // 64-channel (128-byte) column blocks
-  static constexpr int kQBufs = 2;
-  static constexpr int kStages = D == 64 ? 8 : 3;      // of 64 keys: 128 / 96 KB of K and V
-  static constexpr int kThreads = 128 + 128 * kChains;
-  static constexpr int kCtrlRegs = kChains == 3 ? 56 : 80;
-  static constexpr int kSoftRegs = kChains == 3 ? 152 : 208;
-  static_assert(128 * kCtrlRegs + 128 * kChains * kSoftRegs <= 65536, "register split");
-  // TMEM columns: S_c (fp32), O_c (fp32), P_c (16-bit pairs) of every chain.
-  static constexpr uint32_t kColS = 0, kColO = kChains * kBN, kColP = kColO + kChains * D;
-  static_assert(kColP + kChains * kBN / 2 <= 512, "TMEM columns");
-};
-
-template <int D>
 struct TileSmem {
   using C = Cfg<D>;
-  uint16_t q[C::kQBufs][C::kChains][C::kHalves][kBM * 64];  // this item's and the next one's
-  uint16_t k[C::kStages][C::kHalves][kBN * 64];
-  uint16_t v[C::kStages][C::kHalves][kBN * 64];
-  uint64_t q_full[C::kQBufs], q_empty[C::kQBufs];
-  uint64_t k_full[C::kStages], v_full[C::kStages], kv_empty[C::kStages];
+  uint16_t q[C::kQTiles][C::kHalves][kBM * 64];
+  uint16_t k[C::kStages][C::kHalves][C::kBN * 64];
+  uint16_t v[C::kStages][C::kHalves][C::kBN * 64];
+  uint64_t q_full[C::kQTiles], q_empty[C::kQTiles];
+  uint64_t k_full[C::kStages], v_full[C::kStages], k_empty[C::kStages], v_empty[C::kStages];
   uint64_t s_full[C::kChains], s_empty[C::kChains], p_full[C::kChains], o_bar[C::kChains],
-      o_empty[C::kChains], drain[C::kChains];
+      o_empty[C::kChains], drain[C::kChains], turn[C::kChains];
+  uint64_t staged[C::kChains][2];  // an item's outputs of a chain are in its Q tile (items in turn)
   uint32_t tmem_base;
   int abort_flag;
   int nonfinite[2];  // V values of masked tiles replaced by 0: any, and any that some row sees
@@ -214,9 +226,10 @@ __device__ __forceinline__ long long cta_scan(long long v, long long* s_warp, lo
 // The units of all tiles in order, summed up tile by tile: fn(b, c0, seq, extent of an item,
 // extent before the tile) for every tile, each on one thread.  Returns the total.  Called by all threads;
 // s_seq, s_off: scratch for blockDim sequences.
-template <int kChains, class Fn>
+template <class C, class Fn>
 __device__ __forceinline__ long long scan_tiles(const SeqAttnArgs& a, int4* s_seq, long long* s_warp,
                                                 Fn fn) {
+  constexpr int kChains = C::kChains;
   const int tid = threadIdx.x, n = blockDim.x;
   long long before = 0;
   for (int b0 = 0; b0 < a.B; b0 += n) {
@@ -242,7 +255,7 @@ __device__ __forceinline__ long long scan_tiles(const SeqAttnArgs& a, int4* s_se
         const int4 x = s_seq[lo];
         s = Seq{x.x, x.y, x.z};
         c0 = (w - (x.w - ceil_div(count_chains(a, s.ql), kChains))) * kChains;
-        u = tile_units<kChains>(a, c0, s) + kItemCost;
+        u = tile_units<C>(a, c0, s) + C::kItemCost;
       }
       long long total;
       const long long upto = cta_scan(u * a.Hkv, s_warp, &total);
@@ -283,32 +296,36 @@ __device__ __forceinline__ bool chain_any(int c, bool v) {
   return r != 0;
 }
 
-// Replaces what is not finite in the 64 V rows of a tile by 0 (the chain's 128 threads, 16 bytes
-// each in turn).  flags[0]: there was something to replace; flags[1]: in a row below n_valid.
-template <int D, bool F16>
-__device__ __forceinline__ void scrub_v(uint16_t* v, int n_valid, int tid, volatile int* flags) {
-  constexpr int kVecs = kBN * D / 8 / 128;
+// Replaces what is not finite in the rows [first, kBN) of a V tile by 0 (the chain's 128 threads,
+// 16 rows at a time).  flags[0]: there was something to replace; flags[1]: in a row below n_valid.
+template <int D, int kBN, bool F16>
+__device__ __forceinline__ void scrub_v(uint16_t* v, int first, int n_valid, int tid, volatile int* flags) {
+  constexpr int kHalves = D / 64;
   uint4* p = reinterpret_cast<uint4*>(v);
-  uint4 x[kVecs];
-  bool bad = false;
+  // In pairs of passes, so that two loads or more are in flight.
+#pragma unroll 1
+  for (int r0 = first / 32 * 32; r0 < kBN; r0 += 32) {
+    uint4 x[2 * kHalves];
+    bool bad = false;
 #pragma unroll
-  for (int i = 0; i < kVecs; ++i) {
-    x[i] = p[tid + 128 * i];
-    bad |= nonfinite2<F16>(x[i].x) || nonfinite2<F16>(x[i].y) || nonfinite2<F16>(x[i].z) ||
-           nonfinite2<F16>(x[i].w);
-  }
-  if (bad) {
+    for (int i = 0; i < 2 * kHalves; ++i) {
+      x[i] = p[(i >> 1) * (kBN * 8) + (r0 + 16 * (i & 1)) * 8 + tid];
+      bad |= nonfinite2<F16>(x[i].x) || nonfinite2<F16>(x[i].y) || nonfinite2<F16>(x[i].z) ||
+             nonfinite2<F16>(x[i].w);
+    }
+    if (bad) {
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      const int e = tid + 128 * i;
-      if (!(nonfinite2<F16>(x[i].x) || nonfinite2<F16>(x[i].y) || nonfinite2<F16>(x[i].z) ||
-            nonfinite2<F16>(x[i].w)))
-        continue;
-      flags[0] = 1;
-      if (((e >> 3) & (kBN - 1)) < n_valid) flags[1] = 1;  // rows of 8 vectors, kBN rows a half
-      __threadfence_block();
-      p[e] = make_uint4(finite2<F16>(x[i].x), finite2<F16>(x[i].y), finite2<F16>(x[i].z),
-                        finite2<F16>(x[i].w));
+      for (int i = 0; i < 2 * kHalves; ++i) {
+        const int row = r0 + 16 * (i & 1) + (tid >> 3);
+        if (!(nonfinite2<F16>(x[i].x) || nonfinite2<F16>(x[i].y) || nonfinite2<F16>(x[i].z) ||
+              nonfinite2<F16>(x[i].w)))
+          continue;
+        flags[0] = 1;
+        if (row < n_valid) flags[1] = 1;
+        __threadfence_block();
+        p[(i >> 1) * (kBN * 8) + (r0 + 16 * (i & 1)) * 8 + tid] =
+            make_uint4(finite2<F16>(x[i].x), finite2<F16>(x[i].y), finite2<F16>(x[i].z), finite2<F16>(x[i].w));
+      }
     }
   }
   // Zeros written here, or by another chain's threads and read here: before this chain's MMA.
@@ -356,16 +373,17 @@ __device__ __noinline__ void refill_part(const SeqAttnArgs& a, const Item& it, i
 
 // This CTA's run, into *run (visible after the next barrier), and its entry of the list of cut
 // items: an item whose first part is this run's end.
-template <int kChains>
+template <class C>
 __device__ __forceinline__ void find_run(const SeqAttnArgs& a, const SeqScratch& sc, int4* s_seq,
                                          Run* run) {
+  constexpr int kItemCost = C::kItemCost;
   __shared__ long long s_warp[32], s_begin, s_end, s_first;
   __shared__ int4 s_rec[2];
   const int P = gridDim.x, cta = blockIdx.x;
   if (threadIdx.x == 0) {
     s_rec[0] = make_int4(0, 0, 0, 0);
   }
-  const long long total = scan_tiles<kChains>(a, s_seq, s_warp, [](int, int, const Seq&, int, long long) {});
+  const long long total = scan_tiles<C>(a, s_seq, s_warp, [](int, int, const Seq&, int, long long) {});
   const long long per = (total + P - 1) / P, near = max(per / 16, kItemCost + 4ll);
   const long long x0 = cta * per, x1 = x0 + per;
   if (threadIdx.x == 0) {
@@ -373,7 +391,7 @@ __device__ __forceinline__ void find_run(const SeqAttnArgs& a, const SeqScratch&
     s_end = min(x1, total);
     run->b = run->c0 = run->h = run->j0 = 0;
   }
-  scan_tiles<kChains>(a, s_seq, s_warp, [&](int b, int c0, const Seq& s, int n, long long before) {
+  scan_tiles<C>(a, s_seq, s_warp, [&](int b, int c0, const Seq& s, int n, long long before) {
     const long long end = before + (long long)n * a.Hkv;
     if (before <= x0 && x0 < end) {
       const int h = (int)((x0 - before) / n);
@@ -413,8 +431,9 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
                     const __grid_constant__ CUtensorMap tmap_out,
                     const __grid_constant__ SeqAttnArgs prm, const SeqScratch sc) {
   using C = Cfg<D>;
-  constexpr int kChains = C::kChains, kStages = C::kStages, kHalves = C::kHalves;
-  constexpr uint32_t kQBufs = C::kQBufs;
+  constexpr int kChains = C::kChains, kStages = C::kStages, kHalves = C::kHalves, kBN = C::kBN;
+  constexpr uint32_t kQTiles = C::kQTiles;
+  constexpr bool kAlias = C::kAlias, kStoreWarp = C::kChains < 3;  // warp 3 is free with two chains
   extern __shared__ unsigned char smem_raw[];
   TileSmem<D>& sm = *reinterpret_cast<TileSmem<D>*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -423,18 +442,19 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
   volatile int* abort_flag = &sm.abort_flag;
   unsigned int* err = prm.err;
   pdl_launch_dependents();
-  find_run<kChains>(prm, sc, reinterpret_cast<int4*>(sm.q), &sm.run);
+  find_run<C>(prm, sc, reinterpret_cast<int4*>(sm.q), &sm.run);
   fence_proxy_async_smem();  // sm.q was scratch: before the copies into it
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < C::kQBufs; ++s) {
+    for (int s = 0; s < C::kQTiles; ++s) {
       mbar_init(&sm.q_full[s], 1);
-      mbar_init(&sm.q_empty[s], 2 * kChains);  // every chain's last scores and epilogue
+      mbar_init(&sm.q_empty[s], 2);  // the chain's last scores and its epilogue
     }
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&sm.k_full[s], 1);
       mbar_init(&sm.v_full[s], 1);
-      mbar_init(&sm.kv_empty[s], kChains);
+      mbar_init(&sm.k_empty[s], kChains);
+      mbar_init(&sm.v_empty[s], kChains);
     }
     for (int c = 0; c < kChains; ++c) {
       mbar_init(&sm.s_full[c], 1);
@@ -443,6 +463,9 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       mbar_init(&sm.o_bar[c], 1);
       mbar_init(&sm.o_empty[c], 128);
       mbar_init(&sm.drain[c], 1);
+      mbar_init(&sm.turn[c], 1);
+      mbar_init(&sm.staged[c][0], 128);
+      mbar_init(&sm.staged[c][1], 128);
     }
     sm.abort_flag = 0;
     sm.nonfinite[0] = sm.nonfinite[1] = 0;
@@ -467,37 +490,50 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
   if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kCtrlRegs));
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
-    uint32_t lc = 0, ic = 0;
+    uint32_t lc = 0, ic = 0, qk = 0, k_ahead = 0;  // tiles, items, Q tiles; 1: K of tile lc is on its way
     bool ok = true;
     const int log2p = prm.kv.log2_page, ps = prm.kv.page_size;
     const int ppt = kPaged ? (ps >= kBN ? 1 : kBN / ps) : 1;  // pages (boxes) of a tile
     const uint32_t box_bytes = (kPaged && ps < kBN ? ps : kBN) * 128;
-    Walk<kChains> walk;
+    Walk<C> walk;
     for (walk.start(prm, sm.run);; walk.next(prm), ++ic) {
       const Item& it = walk.it;
-      const int qb = ic % kQBufs;
-      ok = mbar_wait_warp(&sm.q_empty[qb], ((ic / kQBufs) & 1) ^ 1, err, abort_flag);
-      if (!ok) break;
-      if (walk.left <= 0) {  // the end of the run
-        if (lane == 0) {
-          sm.item[ic % kItemRing].nk = -1;
-          mbar_arrive(&sm.q_full[qb]);
+      // Q of chains c .. c_end - 1 (nothing to load for a chain without tokens), in turn.
+      auto load_q = [&](int c, int c_end) {
+        for (; c < c_end && ok; ++c) {
+          const uint32_t qb = qk % kQTiles;
+          ok = mbar_wait_warp(&sm.q_empty[qb], ((qk / kQTiles) & 1) ^ 1, err, abort_flag);
+          if (!ok) return;
+          if (c == 0) {  // the item's first Q tile: publish it
+            if (lane == 0) {
+              sm.item[ic % kItemRing] = it;
+              if (walk.left <= 0) sm.item[ic % kItemRing].nk = -1;  // the end of the run
+            }
+            if (lane < kChains && walk.left > 0)
+              sm.chain[ic % kItemRing][lane] = chain_of<kBN>(prm, it, lane, walk.n_chains);
+            __syncwarp();
+          }
+          if (elect_one()) {
+            if (walk.left > 0 && it.c0 + c < walk.n_chains) {
+              mbar_arrive_expect_tx(&sm.q_full[qb], kHalves * tpt * group * 128);
+#pragma unroll
+              for (int hf = 0; hf < kHalves; ++hf)
+                tma_load_4d(sm.q[qb][hf], &tmap_q, &sm.q_full[qb], hf * 64, 0, it.h,
+                            it.q0 + chain_start(prm, it.c0 + c));
+            } else {
+              mbar_arrive(&sm.q_full[qb]);
+            }
+          }
+          __syncwarp();
+          ++qk;
         }
+      };
+      load_q(0, 1);
+      if (!ok) break;
+      if (walk.left <= 0) {
+        load_q(1, kChains);
         break;
       }
-      const int chains = min(kChains, walk.n_chains - it.c0);
-      if (lane == 0) sm.item[ic % kItemRing] = it;
-      if (lane < kChains) sm.chain[ic % kItemRing][lane] = chain_of(prm, it, lane, walk.n_chains);
-      __syncwarp();
-      if (elect_one()) {
-        mbar_arrive_expect_tx(&sm.q_full[qb], chains * kHalves * tpt * group * 128);
-        for (int c = 0; c < chains; ++c)
-#pragma unroll
-          for (int hf = 0; hf < kHalves; ++hf)
-            tma_load_4d(sm.q[qb][c][hf], &tmap_q, &sm.q_full[qb], hf * 64, 0, it.h,
-                        it.q0 + chain_start(prm, it.c0 + c));
-      }
-      __syncwarp();
       // Page ids: lane l holds that of page first + l; `next` the 32 after them.
       const int n_pages = kPaged ? (it.kl + ps - 1) >> log2p : 0;
       const int32_t* table = kPaged ? prm.kv.table + (size_t)it.b * prm.kv.width : nullptr;
@@ -521,57 +557,173 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
           y = (j * kBN) & (ps - 1);
           if (lane < n_box && (unsigned)page >= (unsigned)prm.kv.n_pages) atomicOr(err, VP_DEVERR_PAGE);
         }
-        ok = mbar_wait_warp(&sm.kv_empty[st], ((lc / kStages) & 1) ^ 1, err, abort_flag);
+        const uint32_t par = ((lc / kStages) & 1) ^ 1;
+        const int off = lane * (box_bytes / 2);
+        if (kAlias) {
+          ok = mbar_wait_warp(&sm.k_empty[st], par, err, abort_flag);
+        } else {  // K and V of a tile are released together
+          ok = mbar_wait_warp(&sm.v_empty[st], par, err, abort_flag);
+        }
         if (!ok) break;
         if (lane == 0) {
           mbar_arrive_expect_tx(&sm.k_full[st], n_box * kHalves * box_bytes);
-          mbar_arrive_expect_tx(&sm.v_full[st], n_box * kHalves * box_bytes);
+          if (!kAlias) mbar_arrive_expect_tx(&sm.v_full[st], n_box * kHalves * box_bytes);
         }
         __syncwarp();
-        if (lane < n_box) {
-          const int off = lane * (box_bytes / 2);
+        if (lane < n_box)
 #pragma unroll
           for (int hf = 0; hf < kHalves; ++hf)
             tma_load_4d(sm.k[st][hf] + off, &tmap_k, &sm.k_full[st], hf * 64, y, it.h, page);
+        if (kAlias) {
+          ok = mbar_wait_warp(&sm.v_empty[st], par, err, abort_flag);
+          if (!ok) {
+            k_ahead = 1;
+            break;
+          }
+          if (lane == 0) mbar_arrive_expect_tx(&sm.v_full[st], n_box * kHalves * box_bytes);
+          __syncwarp();
+        }
+        if (lane < n_box)
 #pragma unroll
           for (int hf = 0; hf < kHalves; ++hf)
             tma_load_4d(sm.v[st][hf] + off, &tmap_v, &sm.v_full[st], hf * 64, y, it.h, page);
-        }
         __syncwarp();
+        if (jj == 0) {  // the other chains' Q behind the first keys
+          load_q(1, kChains);
+          if (!ok) {
+            ++lc;
+            break;
+          }
+        }
       }
       if (!ok) break;
     }
     if (!ok && lane == 0) {
-      // Let the copies this warp issued land before the CTA releases its shared memory.
-      for (uint32_t i = ic > kQBufs ? ic - kQBufs : 0; i <= ic; ++i)
-        for (int t = 0; t < 1000000 && !mbar_try_wait(&sm.q_full[i % kQBufs], (i / kQBufs) & 1); ++t) {}
-      for (int s = 0; s < kStages; ++s) {
-        if (lc > (uint32_t)s) {
-          const uint32_t last = (lc - 1 - s) / kStages * kStages + s;  // last use of stage s
-          const uint32_t par = (last / kStages) & 1;
-          for (int t = 0; t < 1000000 && !mbar_try_wait(&sm.k_full[s], par); ++t) {}
-          for (int t = 0; t < 1000000 && !mbar_try_wait(&sm.v_full[s], par); ++t) {}
-        }
+      // Let the copies this warp issued land before the CTA releases its shared memory: the last use
+      // of slot s of a ring of n after `count` uses.
+      auto wait_last = [&](uint64_t* bar, uint32_t s, uint32_t n, uint32_t count) {
+        if (count <= s) return;
+        const uint32_t last = (count - 1 - s) / n * n + s;
+        for (int t = 0; t < 1000000 && !mbar_try_wait(bar, (last / n) & 1); ++t) {}
+      };
+      for (uint32_t s = 0; s < kQTiles; ++s) wait_last(&sm.q_full[s], s, kQTiles, qk);
+      for (uint32_t s = 0; s < (uint32_t)kStages; ++s) {
+        wait_last(&sm.k_full[s], s, kStages, lc + k_ahead);
+        wait_last(&sm.v_full[s], s, kStages, lc);
       }
     }
-  } else if (warp <= kChains) {
+  } else if (kAlias && warp <= kChains) {
+    // ------------------------------------------------------------ MMA issuers (chain c), by turns
+    // A chain's products of a step, P_c V of this tile and S_c of the next, are issued in one go and
+    // the chains take turns, so that one chain's softmax runs while the other's MMAs do; without
+    // turns the two interleave and both softmaxes run at once (3,880 clocks for 2 x 128 rows x
+    // 128 keys of d 128, against 2,048 of MMAs).  A warp per chain: the waits of one (a couple of
+    // hundred clocks even when there is nothing to wait for) pass during the other's turn.
+    const int c = warp - 1;
+    const uint32_t id_s = idesc_16bit<F16>(kBM, kBN, 0);  // Q (K-major) x K^T (K-major)
+    const uint32_t id_o = idesc_16bit<F16>(kBM, 64, 1);   // P (TMEM) x V (MN-major)
+    const uint32_t t_s = tmem + C::kColS + c * kBN;
+    const uint32_t t_o = tmem + C::kColO + c * D;
+    const uint32_t t_p = tmem + C::kColP + c * C::kPitchP;
+    uint32_t lc = 0, g = 0, oc = 0, turn = 0;  // ring tiles, this chain's tiles, its items, its turns
+    bool ok = true;
+    // Three barriers at once (lanes 0-10, 11-21, 22-31).
+    auto wait3 = [&](uint64_t* b0, uint32_t p0, uint64_t* b1, uint32_t p1, uint64_t* b2, uint32_t p2) {
+      const int grp = lane / 11;
+      uint64_t* bar = grp == 0 ? b0 : grp == 1 ? b1 : b2;
+      const uint32_t par = grp == 0 ? p0 : grp == 1 ? p1 : p2;
+      return (bool)__all_sync(0xffffffffu, mbar_wait(bar, par, err, abort_flag));
+    };
+    auto my_turn = [&] { return c == 0 ? (turn & 1) ^ 1 : turn & 1; };
+    for (uint32_t ic = 0;; ++ic) {
+      const uint32_t qi = ic * kChains + c, qb = qi % kQTiles;
+      ok = mbar_wait_warp(&sm.q_full[qb], (qi / kQTiles) & 1, err, abort_flag);
+      if (!ok) break;
+      const int nk = uniform(sm.item[ic % kItemRing].nk);
+      const int n = uniform(sm.chain[ic % kItemRing][c].n);
+      if (nk < 0) break;
+      const uint64_t dq = sdesc_sw128(smem_u32(sm.q[qb][0]));
+      // Step -1: S_c(0); step j: P_c(j) V and S_c(j + 1).
+      for (int j = -1; j < nk && ok; ++j) {
+        const uint32_t l = lc + j;  // the ring's tile of P V; l + 1 that of S
+        const int st = l % kStages, st1 = (l + 1) % kStages;
+        const bool pv = j >= 0 && j < n, sc_next = j + 1 < n;
+        uint64_t* k_bar = &sm.k_full[st1];
+        const uint32_t k_par = ((l + 1) / kStages) & 1, v_par = (l / kStages) & 1;
+        if (pv)
+          ok = wait3(&sm.p_full[c], g & 1, &sm.v_full[st], v_par, sc_next ? k_bar : &sm.p_full[c],
+                     sc_next ? k_par : g & 1);
+        else if (sc_next)
+          ok = mbar_wait_warp(k_bar, k_par, err, abort_flag);
+        else if (j >= 0)  // past the chain's last visible key: released once it has landed
+          ok = mbar_wait_warp(&sm.k_full[st], v_par, err, abort_flag) &&
+               mbar_wait_warp(&sm.v_full[st], v_par, err, abort_flag);
+        if (ok && pv && j == 0) ok = mbar_wait_warp(&sm.o_empty[c], (oc & 1) ^ 1, err, abort_flag);
+        ok = ok && mbar_wait_warp(&sm.turn[c], my_turn(), err, abort_flag);
+        if (!ok) break;
+        ++turn;
+        tc_fence_after();
+        const uint64_t dv = sdesc_sw128(smem_u32(sm.v[st][0]));
+        const uint64_t dk = sdesc_sw128(smem_u32(sm.k[st1][0]));
+        if (elect_one()) {
+          if (pv) {
+#pragma unroll
+            for (int kk = 0; kk < kBN / 16; ++kk)  // 16 keys per step: 8 TMEM columns, 2 KB of V
+#pragma unroll
+              for (int hf = 0; hf < kHalves; ++hf)
+                tc_mma_ts(t_o + 64 * hf, t_p + 8 * kk,
+                          dv + hf * (kBN * 128 / 16) + (uint64_t)(kk * 128), id_o,
+                          (j > 0 || kk > 0) ? 1u : 0u);
+            tc_commit(&sm.v_empty[st]);
+            if (j == n - 1) tc_commit(&sm.o_bar[c]);
+          } else if (j >= 0) {
+            mbar_arrive(&sm.k_empty[st]);
+            mbar_arrive(&sm.v_empty[st]);
+          }
+          if (sc_next) {
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk)  // K = 16 per step: +32 bytes, +1 block per 64
+              tc_mma_ss(t_s, dq + (kk >> 2) * (kBM * 128 / 16) + 2 * (kk & 3),
+                        dk + (kk >> 2) * (kBN * 128 / 16) + 2 * (kk & 3), id_s, kk > 0);
+            tc_commit(&sm.s_full[c]);
+            tc_commit(&sm.k_empty[st1]);
+            if (j + 1 == n - 1) tc_commit(&sm.q_empty[qb]);
+          }
+          if (j < 0 && n == 0) mbar_arrive(&sm.q_empty[qb]);
+          mbar_arrive(&sm.turn[c ^ 1]);
+        }
+        __syncwarp();
+        if (pv) ++g;
+      }
+      if (!ok) break;
+      lc += nk;
+      oc += n > 0;
+    }
+    if (!ok) {
+      if (elect_one()) {
+        tc_commit(&sm.drain[c]);
+        for (int t = 0; t < 1000000 && !mbar_try_wait(&sm.drain[c], 0); ++t) {}
+      }
+      __syncwarp();
+    }
+  } else if (!kAlias && warp <= kChains) {
     // ------------------------------------------------------------ MMA issuers (chain c)
     const int c = warp - 1;
     const uint32_t id_s = idesc_16bit<F16>(kBM, kBN, 0);  // Q (K-major) x K^T (K-major)
     const uint32_t id_o = idesc_16bit<F16>(kBM, 64, 1);   // P (TMEM) x V (MN-major)
     const uint32_t t_s = tmem + C::kColS + c * kBN;
     const uint32_t t_o = tmem + C::kColO + c * D;
-    const uint32_t t_p = tmem + C::kColP + c * (kBN / 2);
+    const uint32_t t_p = tmem + C::kColP + c * C::kPitchP;
     uint32_t lc = 0, ic = 0, g = 0, oc = 0;  // ring tiles, items, this chain's tiles, its items
     bool ok = true;
     for (;; ++ic) {
-      const int qb = ic % kQBufs;
-      ok = mbar_wait_warp(&sm.q_full[qb], (ic / kQBufs) & 1, err, abort_flag);
+      const uint32_t qi = ic * kChains + c, qb = qi % kQTiles;
+      ok = mbar_wait_warp(&sm.q_full[qb], (qi / kQTiles) & 1, err, abort_flag);
       if (!ok) break;
-      const Item& it = sm.item[ic % kItemRing];
-      const int nk = it.nk, n = sm.chain[ic % kItemRing][c].n;
+      const int nk = uniform(sm.item[ic % kItemRing].nk);
+      const int n = uniform(sm.chain[ic % kItemRing][c].n);
       if (nk < 0) break;
-      const uint64_t dq = sdesc_sw128(smem_u32(sm.q[qb][c][0]));
+      const uint64_t dq = sdesc_sw128(smem_u32(sm.q[qb][0]));
       tc_fence_after();
       const uint32_t lc0 = lc, g0 = g;
       auto issue_s = [&](int j) -> bool {
@@ -618,7 +770,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
               tc_mma_ts(t_o + 64 * hf, t_p + 8 * kk, dv + hf * (kBN * 128 / 16) + (uint64_t)(kk * 128),
                         id_o, (j > 0 || kk > 0) ? 1u : 0u);
           tc_commit(&sm.o_bar[c]);
-          tc_commit(&sm.kv_empty[st]);
+          tc_commit(&sm.v_empty[st]);
         }
         __syncwarp();
       }
@@ -628,7 +780,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
         const int st = l % kStages;
         ok = mbar_wait_warp(&sm.k_full[st], (l / kStages) & 1, err, abort_flag) &&
              mbar_wait_warp(&sm.v_full[st], (l / kStages) & 1, err, abort_flag);
-        if (ok && lane == 0) mbar_arrive(&sm.kv_empty[st]);
+        if (ok && lane == 0) mbar_arrive(&sm.v_empty[st]);  // of K and V
       }
       if (!ok) break;
       lc = lc0 + nk;
@@ -642,6 +794,37 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       }
       __syncwarp();
     }
+  } else if (kStoreWarp && warp == 3) {
+    // ------------------------------------------------------------ stores of staged outputs
+    bool ok = true;
+    for (uint32_t ic = 0; ok; ++ic) {
+      int nk = 0;
+      for (int c = 0; c < kChains && ok && nk >= 0; ++c) {
+        const uint32_t qi = ic * kChains + c, qb = qi % kQTiles;
+        ok = mbar_wait_warp(&sm.q_full[qb], (qi / kQTiles) & 1, err, abort_flag);
+        if (!ok) break;
+        const Item& it = sm.item[ic % kItemRing];
+        nk = it.nk;
+        if (nk < 0) break;
+        ok = mbar_wait_warp(&sm.staged[c][ic & 1], (ic >> 1) & 1, err, abort_flag);
+        if (!ok) break;
+        const Chain ch = sm.chain[ic % kItemRing][c];
+        if (elect_one()) {
+          if (it.nk == it.all && ch.t1 - ch.t0 == tpt) {
+#pragma unroll
+            for (int hf = 0; hf < kHalves; ++hf)
+              tma_store_4d(&tmap_out, sm.q[qb][hf], hf * 64, 0, it.h, it.q0 + ch.t0);
+            tma_store_commit();
+            tma_store_wait_read<0>();
+          }
+          mbar_arrive(&sm.q_empty[qb]);
+        }
+        __syncwarp();
+      }
+      if (nk < 0) break;
+    }
+    if (elect_one()) tma_store_wait_all();
+    __syncwarp();
   } else if (warp >= 4) {
     // ------------------------------------------------------------ softmax / epilogue
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kSoftRegs));
@@ -651,15 +834,16 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
     const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
     const uint32_t t_s = tmem + lane_off + C::kColS + c * kBN;
     const uint32_t t_o = tmem + lane_off + C::kColO + c * D;
-    const uint32_t t_p = tmem + lane_off + C::kColP + c * (kBN / 2);
+    const uint32_t t_p = tmem + lane_off + C::kColP + c * C::kPitchP;
     const int row_tok = row / group, row_head = row - row_tok * group;
     const bool flip = prm.scale_log2 < 0.f;  // scores are negated, so that the maximum is the scores'
     const float cs = fmaxf(fabsf(prm.scale_log2), 1e-30f);
-    uint32_t g = 0, lc = 0;
-    int owed = -1;  // item whose Q tile the copy of its outputs may still be reading (one thread)
+    uint32_t g = 0, lc = 0, oc = 0;  // the chain's tiles, ring tiles, the chain's items
+    int owed = -1;  // Q tile that the copy of an item's outputs may still be reading (one thread)
     bool ok = true;
     for (uint32_t ic = 0;; ++ic) {
-      ok = mbar_wait_warp(&sm.q_full[ic % kQBufs], (ic / kQBufs) & 1, err, abort_flag);
+      const uint32_t qi = ic * kChains + c, qb = qi % kQTiles;
+      ok = mbar_wait_warp(&sm.q_full[qb], (qi / kQTiles) & 1, err, abort_flag);
       // A warp that gives up takes its chain along: all four meet here and at the item's end.
       if (chain_any(c, !ok)) break;
       const Item& it = sm.item[ic % kItemRing];
@@ -668,17 +852,18 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       const int n = ch.n, tok = ch.t0 + row_tok;  // this thread's token in its sequence
       const bool valid = row_tok < tpt && tok < ch.t1;
       const int lim = valid ? row_limit(tok, it.ql, it.kl, block) : 0;
-      const int masked_from = ch.masked_from;
+      const int masked_from = ch.hidden_from / kBN;  // the first tile with a hidden key
       const bool active = __any_sync(0xffffffffu, valid);
       float m = kUnset, lsum = 0.f;
-      // The copy of the item before had this item's start to read its Q tile.
+      // The copy of the last item's outputs has had this item's start to read its Q tile.
       auto release_q = [&] {
         if (owed >= 0) {
           tma_store_wait_read<0>();
-          mbar_arrive(&sm.q_empty[owed % kQBufs]);
+          mbar_arrive(&sm.q_empty[owed]);
           owed = -1;
         }
       };
+      if (n == 0) release_q();
       // One key tile; kMasked: some row of the item does not see all of it (uniform over the
       // chains), or the scores are negated.
       auto tile = [&](auto masked_const, int jj) -> bool {
@@ -689,7 +874,8 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
           const int st = l % kStages;
           if (!mbar_wait_warp(&sm.v_full[st], (l / kStages) & 1, err, abort_flag)) return false;
           if (it.j0 + jj >= masked_from)
-            scrub_v<D, F16>(sm.v[st][0], it.kl - (it.j0 + jj) * kBN, row, sm.nonfinite);
+            scrub_v<D, kBN, F16>(sm.v[st][0], max(ch.hidden_from - (it.j0 + jj) * kBN, 0),
+                                 it.kl - (it.j0 + jj) * kBN, row, sm.nonfinite);
         }
         tc_fence_after();
         float s[kBN], pmx[kBN / 32];
@@ -697,8 +883,10 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
         for (int cc = 0; cc < kBN / 32; ++cc) tmem_ld32_max(t_s + 32 * cc, s + 32 * cc, pmx[cc]);
         tmem_wait_ld();
         tc_fence_before();
-        mbar_arrive(&sm.s_empty[c]);  // the MMA warp may overwrite S_c now
-        float mx = fmaxf(pmx[0], pmx[1]);
+        if (!kAlias) mbar_arrive(&sm.s_empty[c]);  // the MMA warp may overwrite S_c now
+        float mx = pmx[0];
+#pragma unroll
+        for (int cc = 1; cc < kBN / 32; ++cc) mx = fmaxf(mx, pmx[cc]);
         const int n_seen = valid ? lim - (it.j0 + jj) * kBN : kBN;
         if (kMasked && __any_sync(0xffffffffu, flip || n_seen < kBN)) {
 #pragma unroll
@@ -742,8 +930,8 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
         }
         const float2 at = fadd2(acc0, acc1);
         lsum = lsum * alpha + (at.x + at.y);
-        // P_c and O_c are free once P_c(g-1) V has completed.
-        if (g > 0) {
+        // P_c and O_c are free once P_c(g-1) V has completed (before S_c(g), where P_c lies in it).
+        if (!kAlias && g > 0) {
           if (!mbar_wait_warp(&sm.o_bar[c], (g - 1) & 1, err, abort_flag)) return false;
           tc_fence_after();
         }
@@ -763,11 +951,10 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive(&sm.p_full[c]);
-        if (jj == 0) release_q();
+        if (!kStoreWarp && jj == 0) release_q();
         ++g;
         return true;
       };
-      if (n == 0) release_q();
       if (active) {
         const int clear = flip ? 0 : min(max(masked_from - it.j0, 0), n);
         int jj = 0;
@@ -781,16 +968,22 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
           ok = mbar_wait_warp(&sm.s_full[c], g & 1, err, abort_flag);
           if (ok && j >= masked_from) {
             ok = mbar_wait_warp(&sm.v_full[st], (l / kStages) & 1, err, abort_flag);
-            if (ok) scrub_v<D, F16>(sm.v[st][0], it.kl - j * kBN, row, sm.nonfinite);
+            if (ok)
+              scrub_v<D, kBN, F16>(sm.v[st][0], max(ch.hidden_from - j * kBN, 0), it.kl - j * kBN, row,
+                                   sm.nonfinite);
           }
           if (!ok) break;
-          mbar_arrive(&sm.s_empty[c]);
-          if (g > 0) ok = mbar_wait_warp(&sm.o_bar[c], (g - 1) & 1, err, abort_flag);
+          if (!kAlias) {
+            mbar_arrive(&sm.s_empty[c]);
+            if (g > 0) ok = mbar_wait_warp(&sm.o_bar[c], (g - 1) & 1, err, abort_flag);
+          }
           if (ok) mbar_arrive(&sm.p_full[c]);
         }
       }
       lc += it.nk;
-      if (n > 0 && ok) ok = mbar_wait_warp(&sm.o_bar[c], (g - 1) & 1, err, abort_flag);
+      if (n > 0 && ok)  // one o_bar per tile, or (kAlias) per item
+        ok = mbar_wait_warp(&sm.o_bar[c], (kAlias ? oc : g - 1) & 1, err, abort_flag);
+      oc += n > 0;
       if (chain_any(c, !ok)) break;
       tc_fence_after();
       const bool part = it.nk < it.all;
@@ -798,7 +991,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       // in one copy, unless the next sequence's rows would be among them.
       const bool staged = !part && ch.t1 - ch.t0 == tpt;
       const float inv = part ? 1.f : lim > 0 ? 1.f / lsum : 0.f;
-      uint16_t* stage = sm.q[ic % kQBufs][c][0];
+      uint16_t* stage = sm.q[qb][0];
       // Rows: of two 64-channel halves, 16-byte chunks in the swizzled order of the staged tile.
       uint16_t* to = staged ? stage + row * 64
                             : prm.out + (int64_t)(it.q0 + tok) * prm.out_stride + (it.h * group + row_head) * D;
@@ -806,29 +999,30 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       const size_t slot_chain = (size_t)(2 * cta + (it.part > 0)) * kChains + c;
       float* to_part = sc.part_o + (slot_chain * (D / 4) * kBM + row) * 4;  // [D / 4][128 rows][4]
 #pragma unroll
-      for (int q = 0; q < D / 32; ++q) {
-        float o[32];
+      for (int hf = 0; hf < kHalves; ++hf) {
+        float o[64];
         if (n > 0) {
-          tmem_ld32(t_o + 32 * q, o);
+          tmem_ld32(t_o + 64 * hf, o);
+          tmem_ld32(t_o + 64 * hf + 32, o + 32);
           tmem_wait_ld();
-          if (q == D / 32 - 1) {
+          if (hf == kHalves - 1) {
             tc_fence_before();
             mbar_arrive(&sm.o_empty[c]);
           }
         } else {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) o[i] = 0.f;
+          for (int i = 0; i < 64; ++i) o[i] = 0.f;
         }
         if (part) {
           if (valid)
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              *reinterpret_cast<float4*>(to_part + (8 * q + i) * (4 * kBM)) =
+            for (int i = 0; i < 16; ++i)
+              *reinterpret_cast<float4*>(to_part + (16 * hf + i) * (4 * kBM)) =
                   make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
         } else if (valid) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<uint4*>(to + (q >> 1) * half_pitch + ((4 * (q & 1) + i) ^ swizzle) * 8) =
+          for (int i = 0; i < 8; ++i)
+            *reinterpret_cast<uint4*>(to + hf * half_pitch + (i ^ swizzle) * 8) =
                 make_uint4(pack2<F16>(o[8 * i] * inv, o[8 * i + 1] * inv),
                            pack2<F16>(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
                            pack2<F16>(o[8 * i + 4] * inv, o[8 * i + 5] * inv),
@@ -837,7 +1031,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       }
       if (n > 0 && valid && *(volatile int*)&sm.nonfinite[1] != 0) {
         // Chains may have taken values out of V from the item's first hidden key on.
-        const int j0 = max(it.j0, sm.chain[ic % kItemRing][0].masked_from) * kBN;
+        const int j0 = max(it.j0, sm.chain[ic % kItemRing][0].hidden_from / kBN) * kBN;
         const int j1 = min(lim, (it.j0 + n) * kBN);
         if (part)
           refill_part<D, F16, kPaged>(prm, it, j0, j1, to_part);
@@ -849,6 +1043,10 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
         prm.lse[(size_t)(it.q0 + tok) * prm.Hq + it.h * group + row_head] =
             lim > 0 ? (m + log2f(lsum)) * 0.69314718055994531f : -INFINITY;
       if (staged) fence_proxy_async_smem();
+      if (kStoreWarp) {
+        mbar_arrive(&sm.staged[c][ic & 1]);
+        continue;
+      }
       chain_barrier(c);
       if (quarter == 0 && lane == 0) {
         if (staged) {
@@ -856,9 +1054,9 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
           for (int hf = 0; hf < kHalves; ++hf)
             tma_store_4d(&tmap_out, stage + hf * (kBM * 64), hf * 64, 0, it.h, it.q0 + ch.t0);
           tma_store_commit();
-          owed = ic;  // Q is free once the copy has read it: waited for in the next item
+          owed = (int)qb;
         } else {
-          mbar_arrive(&sm.q_empty[ic % kQBufs]);
+          mbar_arrive(&sm.q_empty[qb]);
         }
       }
       __syncwarp();
@@ -901,7 +1099,7 @@ cudaError_t launch_tiles(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms
   const uint64_t os[3] = {D, g * D, (uint64_t)a.out_stride};
   e = make_tmap_16bit_4d(&mo, a.out, F16, qd, os, qb);
   if (e != cudaSuccess) return e;
-  e = make_kv_maps(a, kBN, &mk, &mv);
+  e = make_kv_maps(a, C::kBN, &mk, &mv);
   if (e != cudaSuccess) return e;
   const int P = num_sms < kMaxCtas ? num_sms : kMaxCtas;
   constexpr int smem = (int)sizeof(TileSmem<D>) + 1024;
