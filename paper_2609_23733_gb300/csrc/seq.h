@@ -206,16 +206,6 @@ __device__ __forceinline__ void tma_load_4d(void* smem_dst, const void* tmap, ui
       : "memory");
 }
 
-// 4-D tiled store of a box from shared memory (bulk-group completion).
-__device__ __forceinline__ void tma_store_4d(const void* tmap, const void* smem_src, int x, int y, int z,
-                                             int w) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(
-          reinterpret_cast<uint64_t>(tmap)),
-      "r"(smem_u32(smem_src)), "r"(x), "r"(y), "r"(z), "r"(w)
-      : "memory");
-}
-
 __device__ __forceinline__ void pdl_launch_dependents() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }

@@ -56,8 +56,7 @@ struct Cfg {
   static constexpr int kBN = D == 64 ? 64 : 128;       // keys of a tile
   static constexpr bool kAlias = D == 128;             // P lies in the first columns of S
   static constexpr int kHalves = D / 64;               // 64-channel (128-byte) column blocks
-  static constexpr int kQTiles = D == 64 ? 6 : 3;      // Q tiles of chains, in turn: 96 KB
-  static constexpr int kStages = D == 64 ? 8 : 2;      // 128 KB of K and V
+  static constexpr int kStages = D == 64 ? 8 : 2;      // 128 KB of K and V, beside 48 / 64 KB of Q
   static constexpr int kThreads = 128 + 128 * kChains;
   static constexpr int kCtrlRegs = kChains == 3 ? 56 : 80;
   static constexpr int kSoftRegs = kChains == 3 ? 152 : 208;
@@ -120,8 +119,8 @@ __device__ __forceinline__ Chain chain_of(const SeqAttnArgs& a, const Item& it, 
   return x;
 }
 
-// Items in flight between the producer and the epilogues: with two Q buffers, the producer writes
-// item i + 2 after item i's epilogue.
+// Items in flight between the producer and the epilogues: the producer writes item i + 4 when all
+// softmax warps have begun item i + 2 (the first chain's i + 3), i.e. after item i's epilogue.
 constexpr int kItemRing = 4;
 
 // The segments of a run, one after another.
@@ -187,14 +186,14 @@ struct Walk {
 template <int D>
 struct TileSmem {
   using C = Cfg<D>;
-  uint16_t q[C::kQTiles][C::kHalves][kBM * 64];
+  uint16_t q[C::kChains][C::kHalves][kBM * 64];
+  uint4 out[C::kChains][4][32 * 8];  // of each softmax warp: 64 channels of its 32 rows, on their way out
   uint16_t k[C::kStages][C::kHalves][C::kBN * 64];
   uint16_t v[C::kStages][C::kHalves][C::kBN * 64];
-  uint64_t q_full[C::kQTiles], q_empty[C::kQTiles];
+  uint64_t q_full[C::kChains], q_empty[C::kChains];
   uint64_t k_full[C::kStages], v_full[C::kStages], k_empty[C::kStages], v_empty[C::kStages];
   uint64_t s_full[C::kChains], s_empty[C::kChains], p_full[C::kChains], o_bar[C::kChains],
       o_empty[C::kChains], drain[C::kChains], turn[C::kChains];
-  uint64_t staged[C::kChains][2];  // an item's outputs of a chain are in its Q tile (items in turn)
   uint32_t tmem_base;
   int abort_flag;
   int nonfinite[2];  // V values of masked tiles replaced by 0: any, and any that some row sees
@@ -279,23 +278,6 @@ __host__ __device__ constexpr uint32_t idesc_16bit(int M, int N, int b_mn) {
          ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
-// Barriers of a chain's four softmax warps; chain_any: whether v holds on any of their threads.
-__device__ __forceinline__ void chain_barrier(int c) {
-  asm volatile("bar.sync %0, 128;" ::"r"(c + 1) : "memory");
-}
-__device__ __forceinline__ bool chain_any(int c, bool v) {
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.u32 p, %1, 0;\n\t"
-      "bar.red.or.pred q, %2, 128, p;\n\t"
-      "selp.u32 %0, 1, 0, q;\n\t}"
-      : "=r"(r)
-      : "r"((uint32_t)v), "r"(c + 1)
-      : "memory");
-  return r != 0;
-}
-
 // Replaces what is not finite in the rows [first, kBN) of a V tile by 0 (the chain's 128 threads,
 // 16 rows at a time).  flags[0]: there was something to replace; flags[1]: in a row below n_valid.
 template <int D, int kBN, bool F16>
@@ -357,12 +339,10 @@ __device__ __forceinline__ void add_nonfinite(const SeqAttnArgs& a, const Item& 
   }
 }
 template <int D, bool F16, bool kPaged>
-__device__ __noinline__ void refill_out(const SeqAttnArgs& a, const Item& it, int j0, int j1, uint16_t* out,
-                                        int half_pitch, int swizzle) {
-  auto addr = [&](int c) { return out + (c >> 6) * half_pitch + ((((c & 63) >> 3) ^ swizzle) << 3) + (c & 7); };
+__device__ __noinline__ void refill_out(const SeqAttnArgs& a, const Item& it, int j0, int j1, uint16_t* out) {
   add_nonfinite<D, F16, kPaged>(
-      a, it, j0, j1, [&](int c) { return to_float<F16>(*addr(c)); },
-      [&](int c, float x) { *addr(c) = (uint16_t)pack2<F16>(x, 0.f); });
+      a, it, j0, j1, [&](int c) { return to_float<F16>(out[c]); },
+      [&](int c, float x) { out[c] = (uint16_t)pack2<F16>(x, 0.f); });
 }
 template <int D, bool F16, bool kPaged>
 __device__ __noinline__ void refill_part(const SeqAttnArgs& a, const Item& it, int j0, int j1, float* part) {
@@ -428,12 +408,10 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
     seq_tile_kernel(const __grid_constant__ CUtensorMap tmap_q,
                     const __grid_constant__ CUtensorMap tmap_k,
                     const __grid_constant__ CUtensorMap tmap_v,
-                    const __grid_constant__ CUtensorMap tmap_out,
                     const __grid_constant__ SeqAttnArgs prm, const SeqScratch sc) {
   using C = Cfg<D>;
   constexpr int kChains = C::kChains, kStages = C::kStages, kHalves = C::kHalves, kBN = C::kBN;
-  constexpr uint32_t kQTiles = C::kQTiles;
-  constexpr bool kAlias = C::kAlias, kStoreWarp = C::kChains < 3;  // warp 3 is free with two chains
+  constexpr bool kAlias = C::kAlias;
   extern __shared__ unsigned char smem_raw[];
   TileSmem<D>& sm = *reinterpret_cast<TileSmem<D>*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -446,9 +424,9 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
   fence_proxy_async_smem();  // sm.q was scratch: before the copies into it
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < C::kQTiles; ++s) {
-      mbar_init(&sm.q_full[s], 1);
-      mbar_init(&sm.q_empty[s], 2);  // the chain's last scores and its epilogue
+    for (int c = 0; c < kChains; ++c) {
+      mbar_init(&sm.q_full[c], 1);
+      mbar_init(&sm.q_empty[c], 5);  // the chain's last scores; its softmax warps have begun the item
     }
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&sm.k_full[s], 1);
@@ -464,8 +442,6 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       mbar_init(&sm.o_empty[c], 128);
       mbar_init(&sm.drain[c], 1);
       mbar_init(&sm.turn[c], 1);
-      mbar_init(&sm.staged[c][0], 128);
-      mbar_init(&sm.staged[c][1], 128);
     }
     sm.abort_flag = 0;
     sm.nonfinite[0] = sm.nonfinite[1] = 0;
@@ -474,7 +450,6 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
     tma_prefetch_desc(&tmap_q);
     tma_prefetch_desc(&tmap_k);
     tma_prefetch_desc(&tmap_v);
-    tma_prefetch_desc(&tmap_out);
   }
   if (warp == 1) {
     tmem_alloc(&sm.tmem_base, 512);
@@ -490,7 +465,8 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
   if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kCtrlRegs));
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
-    uint32_t lc = 0, ic = 0, qk = 0, k_ahead = 0;  // tiles, items, Q tiles; 1: K of tile lc is on its way
+    uint32_t lc = 0, ic = 0, k_ahead = 0;  // tiles, items; 1: K of tile lc is on its way
+    int q_last = -1;  // the last Q tile asked for: item x kChains + chain
     bool ok = true;
     const int log2p = prm.kv.log2_page, ps = prm.kv.page_size;
     const int ppt = kPaged ? (ps >= kBN ? 1 : kBN / ps) : 1;  // pages (boxes) of a tile
@@ -501,8 +477,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       // Q of chains c .. c_end - 1 (nothing to load for a chain without tokens), in turn.
       auto load_q = [&](int c, int c_end) {
         for (; c < c_end && ok; ++c) {
-          const uint32_t qb = qk % kQTiles;
-          ok = mbar_wait_warp(&sm.q_empty[qb], ((qk / kQTiles) & 1) ^ 1, err, abort_flag);
+          ok = mbar_wait_warp(&sm.q_empty[c], (ic & 1) ^ 1, err, abort_flag);
           if (!ok) return;
           if (c == 0) {  // the item's first Q tile: publish it
             if (lane == 0) {
@@ -515,17 +490,17 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
           }
           if (elect_one()) {
             if (walk.left > 0 && it.c0 + c < walk.n_chains) {
-              mbar_arrive_expect_tx(&sm.q_full[qb], kHalves * tpt * group * 128);
+              mbar_arrive_expect_tx(&sm.q_full[c], kHalves * tpt * group * 128);
 #pragma unroll
               for (int hf = 0; hf < kHalves; ++hf)
-                tma_load_4d(sm.q[qb][hf], &tmap_q, &sm.q_full[qb], hf * 64, 0, it.h,
+                tma_load_4d(sm.q[c][hf], &tmap_q, &sm.q_full[c], hf * 64, 0, it.h,
                             it.q0 + chain_start(prm, it.c0 + c));
             } else {
-              mbar_arrive(&sm.q_full[qb]);
+              mbar_arrive(&sm.q_full[c]);
             }
           }
           __syncwarp();
-          ++qk;
+          q_last = ic * kChains + c;
         }
       };
       load_q(0, 1);
@@ -606,7 +581,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
         const uint32_t last = (count - 1 - s) / n * n + s;
         for (int t = 0; t < 1000000 && !mbar_try_wait(bar, (last / n) & 1); ++t) {}
       };
-      for (uint32_t s = 0; s < kQTiles; ++s) wait_last(&sm.q_full[s], s, kQTiles, qk);
+      for (uint32_t c = 0; c < (uint32_t)kChains; ++c) wait_last(&sm.q_full[c], c, kChains, q_last + 1);
       for (uint32_t s = 0; s < (uint32_t)kStages; ++s) {
         wait_last(&sm.k_full[s], s, kStages, lc + k_ahead);
         wait_last(&sm.v_full[s], s, kStages, lc);
@@ -636,13 +611,12 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
     };
     auto my_turn = [&] { return c == 0 ? (turn & 1) ^ 1 : turn & 1; };
     for (uint32_t ic = 0;; ++ic) {
-      const uint32_t qi = ic * kChains + c, qb = qi % kQTiles;
-      ok = mbar_wait_warp(&sm.q_full[qb], (qi / kQTiles) & 1, err, abort_flag);
+      ok = mbar_wait_warp(&sm.q_full[c], ic & 1, err, abort_flag);
       if (!ok) break;
       const int nk = uniform(sm.item[ic % kItemRing].nk);
       const int n = uniform(sm.chain[ic % kItemRing][c].n);
       if (nk < 0) break;
-      const uint64_t dq = sdesc_sw128(smem_u32(sm.q[qb][0]));
+      const uint64_t dq = sdesc_sw128(smem_u32(sm.q[c][0]));
       // Step -1: S_c(0); step j: P_c(j) V and S_c(j + 1).
       for (int j = -1; j < nk && ok; ++j) {
         const uint32_t l = lc + j;  // the ring's tile of P V; l + 1 that of S
@@ -687,9 +661,9 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
                         dk + (kk >> 2) * (kBN * 128 / 16) + 2 * (kk & 3), id_s, kk > 0);
             tc_commit(&sm.s_full[c]);
             tc_commit(&sm.k_empty[st1]);
-            if (j + 1 == n - 1) tc_commit(&sm.q_empty[qb]);
+            if (j + 1 == n - 1) tc_commit(&sm.q_empty[c]);
           }
-          if (j < 0 && n == 0) mbar_arrive(&sm.q_empty[qb]);
+          if (j < 0 && n == 0) mbar_arrive(&sm.q_empty[c]);
           mbar_arrive(&sm.turn[c ^ 1]);
         }
         __syncwarp();
@@ -717,13 +691,12 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
     uint32_t lc = 0, ic = 0, g = 0, oc = 0;  // ring tiles, items, this chain's tiles, its items
     bool ok = true;
     for (;; ++ic) {
-      const uint32_t qi = ic * kChains + c, qb = qi % kQTiles;
-      ok = mbar_wait_warp(&sm.q_full[qb], (qi / kQTiles) & 1, err, abort_flag);
+      ok = mbar_wait_warp(&sm.q_full[c], ic & 1, err, abort_flag);
       if (!ok) break;
       const int nk = uniform(sm.item[ic % kItemRing].nk);
       const int n = uniform(sm.chain[ic % kItemRing][c].n);
       if (nk < 0) break;
-      const uint64_t dq = sdesc_sw128(smem_u32(sm.q[qb][0]));
+      const uint64_t dq = sdesc_sw128(smem_u32(sm.q[c][0]));
       tc_fence_after();
       const uint32_t lc0 = lc, g0 = g;
       auto issue_s = [&](int j) -> bool {
@@ -739,7 +712,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
             tc_mma_ss(t_s, dq + (kk >> 2) * (kBM * 128 / 16) + 2 * (kk & 3),
                       dk + (kk >> 2) * (kBN * 128 / 16) + 2 * (kk & 3), id_s, kk > 0);
           tc_commit(&sm.s_full[c]);
-          if (j == n - 1) tc_commit(&sm.q_empty[qb]);
+          if (j == n - 1) tc_commit(&sm.q_empty[c]);
         }
         __syncwarp();
         return true;
@@ -747,7 +720,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       if (n > 0) {
         ok = issue_s(0);
       } else if (lane == 0) {
-        mbar_arrive(&sm.q_empty[qb]);
+        mbar_arrive(&sm.q_empty[c]);
       }
       for (int j = 0; j < n && ok; ++j) {
         if (j + 1 < n) {
@@ -794,37 +767,6 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       }
       __syncwarp();
     }
-  } else if (kStoreWarp && warp == 3) {
-    // ------------------------------------------------------------ stores of staged outputs
-    bool ok = true;
-    for (uint32_t ic = 0; ok; ++ic) {
-      int nk = 0;
-      for (int c = 0; c < kChains && ok && nk >= 0; ++c) {
-        const uint32_t qi = ic * kChains + c, qb = qi % kQTiles;
-        ok = mbar_wait_warp(&sm.q_full[qb], (qi / kQTiles) & 1, err, abort_flag);
-        if (!ok) break;
-        const Item& it = sm.item[ic % kItemRing];
-        nk = it.nk;
-        if (nk < 0) break;
-        ok = mbar_wait_warp(&sm.staged[c][ic & 1], (ic >> 1) & 1, err, abort_flag);
-        if (!ok) break;
-        const Chain ch = sm.chain[ic % kItemRing][c];
-        if (elect_one()) {
-          if (it.nk == it.all && ch.t1 - ch.t0 == tpt) {
-#pragma unroll
-            for (int hf = 0; hf < kHalves; ++hf)
-              tma_store_4d(&tmap_out, sm.q[qb][hf], hf * 64, 0, it.h, it.q0 + ch.t0);
-            tma_store_commit();
-            tma_store_wait_read<0>();
-          }
-          mbar_arrive(&sm.q_empty[qb]);
-        }
-        __syncwarp();
-      }
-      if (nk < 0) break;
-    }
-    if (elect_one()) tma_store_wait_all();
-    __syncwarp();
   } else if (warp >= 4) {
     // ------------------------------------------------------------ softmax / epilogue
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kSoftRegs));
@@ -839,15 +781,13 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
     const bool flip = prm.scale_log2 < 0.f;  // scores are negated, so that the maximum is the scores'
     const float cs = fmaxf(fabsf(prm.scale_log2), 1e-30f);
     uint32_t g = 0, lc = 0, oc = 0;  // the chain's tiles, ring tiles, the chain's items
-    int owed = -1;  // Q tile that the copy of an item's outputs may still be reading (one thread)
     bool ok = true;
     for (uint32_t ic = 0;; ++ic) {
-      const uint32_t qi = ic * kChains + c, qb = qi % kQTiles;
-      ok = mbar_wait_warp(&sm.q_full[qb], (qi / kQTiles) & 1, err, abort_flag);
-      // A warp that gives up takes its chain along: all four meet here and at the item's end.
-      if (chain_any(c, !ok)) break;
+      ok = mbar_wait_warp(&sm.q_full[c], ic & 1, err, abort_flag);
+      if (!ok) break;
       const Item& it = sm.item[ic % kItemRing];
       if (it.nk < 0) break;
+      if (lane == 0) mbar_arrive(&sm.q_empty[c]);
       const Chain ch = sm.chain[ic % kItemRing][c];
       const int n = ch.n, tok = ch.t0 + row_tok;  // this thread's token in its sequence
       const bool valid = row_tok < tpt && tok < ch.t1;
@@ -855,15 +795,6 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       const int masked_from = ch.hidden_from / kBN;  // the first tile with a hidden key
       const bool active = __any_sync(0xffffffffu, valid);
       float m = kUnset, lsum = 0.f;
-      // The copy of the last item's outputs has had this item's start to read its Q tile.
-      auto release_q = [&] {
-        if (owed >= 0) {
-          tma_store_wait_read<0>();
-          mbar_arrive(&sm.q_empty[owed]);
-          owed = -1;
-        }
-      };
-      if (n == 0) release_q();
       // One key tile; kMasked: some row of the item does not see all of it (uniform over the
       // chains), or the scores are negated.
       auto tile = [&](auto masked_const, int jj) -> bool {
@@ -951,7 +882,6 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive(&sm.p_full[c]);
-        if (!kStoreWarp && jj == 0) release_q();
         ++g;
         return true;
       };
@@ -984,21 +914,16 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       if (n > 0 && ok)  // one o_bar per tile, or (kAlias) per item
         ok = mbar_wait_warp(&sm.o_bar[c], (kAlias ? oc : g - 1) & 1, err, abort_flag);
       oc += n > 0;
-      if (chain_any(c, !ok)) break;
+      if (!ok) break;
       tc_fence_after();
       const bool part = it.nk < it.all;
-      // The chain's rows go out through its Q tile (no longer needed: o_bar follows the last scores)
-      // in one copy, unless the next sequence's rows would be among them.
-      const bool staged = !part && ch.t1 - ch.t0 == tpt;
       const float inv = part ? 1.f : lim > 0 ? 1.f / lsum : 0.f;
-      uint16_t* stage = sm.q[qb][0];
-      // Rows: of two 64-channel halves, 16-byte chunks in the swizzled order of the staged tile.
-      uint16_t* to = staged ? stage + row * 64
-                            : prm.out + (int64_t)(it.q0 + tok) * prm.out_stride + (it.h * group + row_head) * D;
-      const int half_pitch = staged ? kBM * 64 : 64, swizzle = staged ? row & 7 : 0;
       const size_t slot_chain = (size_t)(2 * cta + (it.part > 0)) * kChains + c;
       float* to_part = sc.part_o + (slot_chain * (D / 4) * kBM + row) * 4;  // [D / 4][128 rows][4]
-#pragma unroll
+      uint16_t* to = prm.out + (int64_t)(it.q0 + tok) * prm.out_stride + (it.h * group + row_head) * D;
+      const unsigned rows = __ballot_sync(0xffffffffu, valid);
+      uint4* out = sm.out[c][quarter];
+#pragma unroll 1
       for (int hf = 0; hf < kHalves; ++hf) {
         float o[64];
         if (n > 0) {
@@ -1019,49 +944,45 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
             for (int i = 0; i < 16; ++i)
               *reinterpret_cast<float4*>(to_part + (16 * hf + i) * (4 * kBM)) =
                   make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-        } else if (valid) {
+          continue;
+        }
+        // Through shared memory (16-byte chunks swizzled by the row), so that eight lanes write a
+        // row's 128 bytes and not every lane 16 of its own row.
+        __syncwarp();
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            *reinterpret_cast<uint4*>(to + hf * half_pitch + (i ^ swizzle) * 8) =
-                make_uint4(pack2<F16>(o[8 * i] * inv, o[8 * i + 1] * inv),
-                           pack2<F16>(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
-                           pack2<F16>(o[8 * i + 4] * inv, o[8 * i + 5] * inv),
-                           pack2<F16>(o[8 * i + 6] * inv, o[8 * i + 7] * inv));
+        for (int i = 0; i < 8; ++i)
+          out[lane * 8 + (i ^ (lane & 7))] =
+              make_uint4(pack2<F16>(o[8 * i] * inv, o[8 * i + 1] * inv),
+                         pack2<F16>(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
+                         pack2<F16>(o[8 * i + 4] * inv, o[8 * i + 5] * inv),
+                         pack2<F16>(o[8 * i + 6] * inv, o[8 * i + 7] * inv));
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int r = 4 * i + (lane >> 3), ch8 = lane & 7;
+          uint16_t* dst = reinterpret_cast<uint16_t*>(
+              __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(to), r));
+          if (rows >> r & 1)
+            *reinterpret_cast<uint4*>(dst + 64 * hf + 8 * ch8) = out[r * 8 + (ch8 ^ (r & 7))];
         }
       }
+      __syncwarp();
       if (n > 0 && valid && *(volatile int*)&sm.nonfinite[1] != 0) {
         // Chains may have taken values out of V from the item's first hidden key on.
         const int j0 = max(it.j0, sm.chain[ic % kItemRing][0].hidden_from / kBN) * kBN;
         const int j1 = min(lim, (it.j0 + n) * kBN);
+        __threadfence_block();  // the row was written by other lanes
         if (part)
           refill_part<D, F16, kPaged>(prm, it, j0, j1, to_part);
         else
-          refill_out<D, F16, kPaged>(prm, it, j0, j1, to, half_pitch, swizzle);
+          refill_out<D, F16, kPaged>(prm, it, j0, j1, to);
       }
       if (valid && part) sc.part_ml[slot_chain * kBM + row] = make_float2(m, lsum);
       if (valid && !part && prm.lse)
         prm.lse[(size_t)(it.q0 + tok) * prm.Hq + it.h * group + row_head] =
             lim > 0 ? (m + log2f(lsum)) * 0.69314718055994531f : -INFINITY;
-      if (staged) fence_proxy_async_smem();
-      if (kStoreWarp) {
-        mbar_arrive(&sm.staged[c][ic & 1]);
-        continue;
-      }
-      chain_barrier(c);
-      if (quarter == 0 && lane == 0) {
-        if (staged) {
-#pragma unroll
-          for (int hf = 0; hf < kHalves; ++hf)
-            tma_store_4d(&tmap_out, stage + hf * (kBM * 64), hf * 64, 0, it.h, it.q0 + ch.t0);
-          tma_store_commit();
-          owed = (int)qb;
-        } else {
-          mbar_arrive(&sm.q_empty[qb]);
-        }
-      }
       __syncwarp();
     }
-    if (quarter == 0 && lane == 0) tma_store_wait_all();
   }
 
   tc_fence_before();
@@ -1089,15 +1010,12 @@ ScratchLayout scratch_layout(int d) {
 template <int D, bool F16, bool kPaged>
 cudaError_t launch_tiles(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms, cudaStream_t st) {
   using C = Cfg<D>;
-  CUtensorMap mq, mk, mv, mo;
+  CUtensorMap mq, mk, mv;
   const uint64_t g = a.group, H = a.Hkv;
   const uint64_t qd[4] = {D, g, H, (uint64_t)a.T};
   const uint64_t qs[3] = {D, g * D, (uint64_t)a.q_stride};
   const uint32_t qb[4] = {64, (uint32_t)g, 1, (uint32_t)a.chain_tokens};
   cudaError_t e = make_tmap_16bit_4d(&mq, a.q, F16, qd, qs, qb);
-  if (e != cudaSuccess) return e;
-  const uint64_t os[3] = {D, g * D, (uint64_t)a.out_stride};
-  e = make_tmap_16bit_4d(&mo, a.out, F16, qd, os, qb);
   if (e != cudaSuccess) return e;
   e = make_kv_maps(a, C::kBN, &mk, &mv);
   if (e != cudaSuccess) return e;
@@ -1106,7 +1024,7 @@ cudaError_t launch_tiles(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms
   const void* tile = reinterpret_cast<const void*>(seq_tile_kernel<D, F16, kPaged>);
   e = cudaFuncSetAttribute(tile, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  seq_tile_kernel<D, F16, kPaged><<<P, C::kThreads, smem, st>>>(mq, mk, mv, mo, a, sc);
+  seq_tile_kernel<D, F16, kPaged><<<P, C::kThreads, smem, st>>>(mq, mk, mv, a, sc);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   return launch_seq_join(a, sc, true, P, st);
