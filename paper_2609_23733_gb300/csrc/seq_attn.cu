@@ -6,7 +6,7 @@
 // (row = token x group + head, so K and V are read once for the group).  The work is the
 // sequence of units (tile, kv head, 64 keys that the tile's last row sees); CTA c of P (one per SM)
 // takes an equal run of them, whatever items (tile, kv head) they belong to, so that all CTAs end
-// together for any mix of lengths (a cut within a sixteenth of a share from an item's end moves
+// together for any mix of lengths (a cut within a 128th of a share from an item's end moves
 // there).  Each CTA finds its run by a scan of the lengths.  An item that a CTA holds
 // in part leaves its unnormalised output; seq_join_kernel (a programmatic dependent launch)
 // joins the parts in order.  Against whole items in descending order with long ones halved (a
@@ -364,7 +364,7 @@ __device__ __forceinline__ void find_run(const SeqAttnArgs& a, const SeqScratch&
     s_rec[0] = make_int4(0, 0, 0, 0);
   }
   const long long total = scan_tiles<C>(a, s_seq, s_warp, [](int, int, const Seq&, int, long long) {});
-  const long long per = (total + P - 1) / P, near = max(per / 16, kItemCost + 4ll);
+  const long long per = (total + P - 1) / P, near = max(per / 128, kItemCost + 4ll);
   const long long x0 = cta * per, x1 = x0 + per;
   if (threadIdx.x == 0) {
     s_begin = min(x0, total);
