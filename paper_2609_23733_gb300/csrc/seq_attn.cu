@@ -1026,7 +1026,9 @@ cudaError_t launch_tiles(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms
   if (e != cudaSuccess) return e;
   seq_tile_kernel<D, F16, kPaged><<<P, C::kThreads, smem, st>>>(mq, mk, mv, a, sc);
   e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
+  // Items of at most kItemCost + 7 key tiles are never cut (find_run): nothing to join.
+  const long long keys = kPaged ? (long long)a.kv.width << a.kv.log2_page : a.T;
+  if (e != cudaSuccess || keys <= (C::kItemCost + 7) * C::kBN) return e;
   return launch_seq_join(a, sc, true, P, st);
 }
 
@@ -1076,6 +1078,31 @@ SeqScratch carve_seq_scratch(void* ws, int d) {
   return s;
 }
 
+namespace {
+
+// Which kernel: the one for few rows reads a sequence's keys again (from L2) for every 16 rows, but
+// starts sooner and spreads a small call over all SMs; the tile kernel reads them once for 384
+// or 256 rows.  The host knows the token and sequence counts and the cache's capacity, not the
+// lengths, so the rule goes by averages.  Measured (us, few rows / tiles; d 64 unless stated):
+//   cache, rows per sequence (token x head of a kv head's group) and keys:
+//     8, 16 x 4,096, 16 kv heads: 51 / 91     32, 16 x 4,096, 4: 21 / 38      32, 64 x 4,096, 4: 57 / 91
+//     64, 16 x 4,096, 4: 31 / 39              128, 1 x 32,768, 4: 31 / 44     128, 16 x 4,096, 4: 51 / 41
+//     64, 16 x 4,096, 16: 140 / 92            128, 4 x 8,192, 2, d 128: 29 / 49
+//   prompts of n tokens, 16 heads and kv heads:
+//     1 x 128: 9.6 / 14.3    1 x 256: 14.2 / 15.6    1 x 512: 20.4 / 18.2    8 x 64: 10.9 / 14.8
+//     8 x 128: 18.2 / 16.2
+bool takes_few_rows(const SeqAttnArgs& a) {
+  const long long rows = (long long)a.T * a.group;            // of a kv head
+  const long long tiles = (long long)a.T * a.Hq / kSmallRows;  // 16-row tiles of all kv heads
+  if (a.kv.k) {
+    const long long keys = (long long)a.kv.width << a.kv.log2_page;  // capacity
+    return rows <= 32ll * a.B || (rows <= 128ll * a.B && tiles * (keys / 64) <= 16000);
+  }
+  return rows <= (long long)kSmallRows * a.B || tiles * ((a.T / a.B + 63) / 64) <= 1200;
+}
+
+}  // namespace
+
 cudaError_t launch_seq_attention(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms,
                                  cudaStream_t st) {
   using Launch = cudaError_t (*)(const SeqAttnArgs&, const SeqScratch&, int, cudaStream_t);
@@ -1085,12 +1112,8 @@ cudaError_t launch_seq_attention(const SeqAttnArgs& a, const SeqScratch& sc, int
       {{launch_tiles<128, false, false>, launch_tiles<128, false, true>},
        {launch_tiles<128, true, false>, launch_tiles<128, true, true>}}};
   prof_before(VP_KERNEL_SEQ_ATTN, st);
-  // Up to 16 rows per sequence on average: the keys are read once by either kernel, and the one for
-  // few rows has more of them in flight and no TMEM round trip; above, it would read them again
-  // for every 16 rows.
-  const bool few = (long long)a.T * a.group <= (long long)kSmallRows * a.B;
-  const cudaError_t e = few ? launch_seq_rows(a, sc, num_sms, st)
-                            : table[a.d == 128][a.fp16 != 0][a.kv.k != nullptr](a, sc, num_sms, st);
+  const cudaError_t e = takes_few_rows(a) ? launch_seq_rows(a, sc, num_sms, st)
+                                          : table[a.d == 128][a.fp16 != 0][a.kv.k != nullptr](a, sc, num_sms, st);
   prof_after(st);
   return e;
 }

@@ -548,6 +548,8 @@ cudaError_t launch_rows(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms,
   seq_rows_kernel<D, F16, kPaged><<<P, kThreads, smem, st>>>(mk, mv, a, sc);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
+  const long long keys = kPaged ? (long long)a.kv.width << a.kv.log2_page : a.T;
+  if (keys <= kBN) return e;  // items of one unit: nothing is cut
   return launch_seq_join(a, sc, false, P, st);
 }
 
