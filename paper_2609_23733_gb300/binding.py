@@ -176,9 +176,17 @@ def _host_p(t):
     return t.data_ptr()
 
 
+# The current stream's handle without building a Stream object (a third of a short call's cost).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream(stream=None):
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is not None and _raw_device is not None and torch.cuda.is_initialized():
+        return _raw_stream(_raw_device())
+    return torch.cuda.current_stream().cuda_stream
 
 
 def dims(N, H=16, d=64, L=64, tau_low=0.01, tau_high=0.20, variant=0) -> VpDims:
@@ -455,25 +463,29 @@ def _rows_p(t, heads, dims, T=None):
     """(address, token stride) of a [T][heads][d] tensor whose heads and channels are contiguous."""
     if t is None:
         return None, 0
-    sh, st = t.shape, t.stride()
-    if len(sh) != 3 or sh[1] != heads or sh[2] != dims.d or (T is not None and sh[0] != T):
-        raise ValueError(f"expected [{'T' if T is None else T}][{heads}][{dims.d}], got {list(sh)}")
-    if st[2] != 1 or (st[1] != dims.d and heads > 1):
+    d = dims.d
+    if t.dim() != 3:
+        raise ValueError(f"expected three dimensions, got {list(t.shape)}")
+    n, h, c = t.shape
+    if h != heads or c != d or (T is not None and n != T):
+        raise ValueError(f"expected [{'T' if T is None else T}][{heads}][{d}], got {list(t.shape)}")
+    s0, s1, s2 = t.stride()
+    if s2 != 1 or (s1 != d and heads > 1):
         raise ValueError("heads and channels must be contiguous")
     if VP_DTYPES.get(t.dtype, -1) != dims.dtype:
         raise ValueError(f"the tensor's type {t.dtype} is not that of dims")
     if not t.is_cuda:
         raise ValueError("device tensors are required (the library has no CPU path)")
     # a single token has no stride of its own: any legal one stands for it
-    return t.data_ptr(), st[0] if sh[0] > 1 else heads * dims.d
+    return t.data_ptr(), s0 if n > 1 else heads * d
 
 
 def _ints_p(t, n, what):
     if t is None:
         return None
-    if t.dtype != torch.int32 or t.numel() != n:
-        raise ValueError(f"{what}: int32 with {n} values")
-    return _p(t)
+    if t.dtype is not torch.int32 or t.numel() != n or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous int32 device tensor with {n} values")
+    return t.data_ptr()
 
 
 def _kv_ref(kv, dims, B):
@@ -501,10 +513,18 @@ def vp_rope_append(dims: VpAttnDims, rope: VpRopeOptions, q, k, v, cu, kv_len, p
                                 0 if ws is None else ws.numel(), _stream(stream)), "vp_rope_append")
 
 
+def _ws_p(ws):
+    if not ws.is_cuda or not ws.is_contiguous() or ws.dtype is not torch.uint8:
+        raise ValueError("ws: a contiguous uint8 device tensor (attn_workspace)")
+    return ws.data_ptr(), ws.numel()
+
+
 def _lse_p(lse, T, dims):
-    if lse is not None and (lse.dtype != torch.float32 or lse.numel() != T * dims.Hq):
-        raise ValueError(f"lse: float32 [{T}][{dims.Hq}]")
-    return _p(lse)
+    if lse is None:
+        return None
+    if lse.dtype is not torch.float32 or lse.numel() != T * dims.Hq or not lse.is_cuda or not lse.is_contiguous():
+        raise ValueError(f"lse: a contiguous float32 device tensor [{T}][{dims.Hq}]")
+    return lse.data_ptr()
 
 
 def vp_prompt_attention(dims: VpAttnDims, q, k, v, cu, out, lse, ws, stream=None):
@@ -514,7 +534,7 @@ def vp_prompt_attention(dims: VpAttnDims, q, k, v, cu, out, lse, ws, stream=None
     vp, vs = _rows_p(v, dims.Hkv, dims, T)
     op, os_ = _rows_p(out, dims.Hq, dims, T)
     _check(lib().vp_prompt_attention(ctypes.byref(dims), T, B, qp, qs, kp, ks, vp, vs, _ints_p(cu, B + 1, "cu"), op,
-                                     os_, _lse_p(lse, T, dims), _p(ws), ws.numel(), _stream(stream)),
+                                     os_, _lse_p(lse, T, dims), *_ws_p(ws), _stream(stream)),
            "vp_prompt_attention")
 
 
@@ -524,7 +544,7 @@ def vp_paged_attention(dims: VpAttnDims, q, cu, kv_len, kv: VpPagedKv, out, lse,
     op, os_ = _rows_p(out, dims.Hq, dims, T)
     _check(lib().vp_paged_attention(ctypes.byref(dims), T, B, qp, qs, _ints_p(cu, B + 1, "cu"),
                                     _ints_p(kv_len, B, "kv_len"), _kv_ref(kv, dims, B), op, os_,
-                                    _lse_p(lse, T, dims), _p(ws), ws.numel(), _stream(stream)), "vp_paged_attention")
+                                    _lse_p(lse, T, dims), *_ws_p(ws), _stream(stream)), "vp_paged_attention")
 
 
 def vp_profile_begin(max_launches: int):

@@ -222,48 +222,60 @@ __device__ __forceinline__ long long cta_scan(long long v, long long* s_warp, lo
   return v;
 }
 
-// The units of all tiles in order, summed up tile by tile: fn(b, c0, seq, extent of an item,
-// extent before the tile) for every tile, each on one thread.  Returns the total.  Called by all threads;
-// s_seq, s_off: scratch for blockDim sequences.
-template <class C, class Fn>
-__device__ __forceinline__ long long scan_tiles(const SeqAttnArgs& a, int4* s_seq, long long* s_warp,
-                                                Fn fn) {
+// The extents of all tiles in order: on_total(sum of them), then fn(b, c0, seq, extent of an item, extent
+// before the tile) for every tile, each on one thread.  One pass over the tiles where there are
+// no more sequences and tiles than threads, else two.  Called by all threads; s_seq, s_warp: scratch
+// for blockDim sequences and warps.
+template <class C, class Total, class Fn>
+__device__ __forceinline__ void scan_tiles(const SeqAttnArgs& a, int4* s_seq, long long* s_warp,
+                                           Total on_total, Fn fn) {
   constexpr int kChains = C::kChains;
   const int tid = threadIdx.x, n = blockDim.x;
-  long long before = 0;
-  for (int b0 = 0; b0 < a.B; b0 += n) {
-    Seq s{0, 0, 0};
-    if (b0 + tid < a.B) s = load_seq(a, b0 + tid);
-    long long tiles;
-    const long long end = cta_scan(ceil_div(count_chains(a, s.ql), kChains), s_warp, &tiles);
-    s_seq[tid] = make_int4(s.q0, s.ql, s.kl, (int)end);  // .w: tiles up to this sequence's last
-    __syncthreads();
-    for (int w0 = 0; w0 < tiles; w0 += n) {
-      const int w = w0 + tid;
-      int lo = 0, c0 = 0;
-      long long u = 0;
-      if (w < tiles) {
-        int hi = min(n, a.B - b0) - 1;  // the first sequence with .w > w
-        while (lo < hi) {
-          const int mid = (lo + hi) >> 1;
-          if (s_seq[mid].w > w)
-            hi = mid;
-          else
-            lo = mid + 1;
+  bool last = false;  // the pass that calls fn
+  for (int pass = 0; pass < 2; ++pass) {
+    long long before = 0;
+    for (int b0 = 0; b0 < a.B; b0 += n) {
+      Seq s{0, 0, 0};
+      if (b0 + tid < a.B) s = load_seq(a, b0 + tid);
+      long long tiles;
+      const long long end = cta_scan(ceil_div(count_chains(a, s.ql), kChains), s_warp, &tiles);
+      s_seq[tid] = make_int4(s.q0, s.ql, s.kl, (int)end);  // .w: tiles up to this sequence's last
+      __syncthreads();
+      const bool once = a.B <= n && tiles <= n;
+      for (int w0 = 0; w0 < tiles; w0 += n) {
+        const int w = w0 + tid;
+        int lo = 0, c0 = 0;
+        long long u = 0;
+        if (w < tiles) {
+          int hi = min(n, a.B - b0) - 1;  // the first sequence with .w > w
+          while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (s_seq[mid].w > w)
+              hi = mid;
+            else
+              lo = mid + 1;
+          }
+          const int4 x = s_seq[lo];
+          s = Seq{x.x, x.y, x.z};
+          c0 = (w - (x.w - ceil_div(count_chains(a, s.ql), kChains))) * kChains;
+          u = tile_units<C>(a, c0, s) + C::kItemCost;
         }
-        const int4 x = s_seq[lo];
-        s = Seq{x.x, x.y, x.z};
-        c0 = (w - (x.w - ceil_div(count_chains(a, s.ql), kChains))) * kChains;
-        u = tile_units<C>(a, c0, s) + C::kItemCost;
+        long long total;
+        const long long upto = cta_scan(u * a.Hkv, s_warp, &total);
+        if (once) {
+          on_total(total);
+          last = true;
+        }
+        if (last && u > 0) fn(b0 + lo, c0, s, (int)u, before + upto - u * a.Hkv);
+        before += total;
       }
-      long long total;
-      const long long upto = cta_scan(u * a.Hkv, s_warp, &total);
-      if (u > 0) fn(b0 + lo, c0, s, (int)u, before + upto - u * a.Hkv);
-      before += total;
+      __syncthreads();
     }
-    __syncthreads();
+    if (last) return;
+    on_total(before);
+    if (before == 0) return;
+    last = true;
   }
-  return before;
 }
 
 // Cut x of the units moved to the end of the item [first, first + n) it lies in, if that is near.
@@ -360,18 +372,21 @@ __device__ __forceinline__ void find_run(const SeqAttnArgs& a, const SeqScratch&
   __shared__ long long s_warp[32], s_begin, s_end, s_first;
   __shared__ int4 s_rec[2];
   const int P = gridDim.x, cta = blockIdx.x;
-  if (threadIdx.x == 0) {
-    s_rec[0] = make_int4(0, 0, 0, 0);
-  }
-  const long long total = scan_tiles<C>(a, s_seq, s_warp, [](int, int, const Seq&, int, long long) {});
-  const long long per = (total + P - 1) / P, near = max(per / 128, kItemCost + 4ll);
-  const long long x0 = cta * per, x1 = x0 + per;
-  if (threadIdx.x == 0) {
-    s_begin = min(x0, total);
-    s_end = min(x1, total);
-    run->b = run->c0 = run->h = run->j0 = 0;
-  }
-  scan_tiles<C>(a, s_seq, s_warp, [&](int b, int c0, const Seq& s, int n, long long before) {
+  long long per = 0, near = 0, x0 = 0, x1 = 0;
+  auto on_total = [&](long long total) {
+    per = (total + P - 1) / P;
+    near = max(per / 128, kItemCost + 4ll);
+    x0 = cta * per;
+    x1 = x0 + per;
+    if (threadIdx.x == 0) {
+      s_begin = min(x0, total);
+      s_end = min(x1, total);
+      s_rec[0] = make_int4(0, 0, 0, 0);
+      run->b = run->c0 = run->h = run->j0 = 0;
+    }
+    __syncthreads();
+  };
+  scan_tiles<C>(a, s_seq, s_warp, on_total, [&](int b, int c0, const Seq& s, int n, long long before) {
     const long long end = before + (long long)n * a.Hkv;
     if (before <= x0 && x0 < end) {
       const int h = (int)((x0 - before) / n);

@@ -20,6 +20,7 @@ constexpr float kUnset = -1e30f;
 template <int D, bool F16, bool kTiles>
 __global__ void __launch_bounds__(kThreads)
     seq_join_kernel(const __grid_constant__ SeqAttnArgs a, const SeqScratch sc) {
+  constexpr int kAtOnce = 4;
   constexpr int kLanes = D / 4, kSub = kTiles ? 1 : 256 / D;
   constexpr int kRowsCta = kThreads / (kLanes * kSub);       // rows of a CTA at a time
   constexpr int kRows = kTiles ? seq_chains(D) * 128 : kSmallRows;  // rows of a slot
@@ -53,21 +54,40 @@ __global__ void __launch_bounds__(kThreads)
     }
     float m = kUnset, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
     if (valid) {
-      for (int i = sub; i < np; i += kSub) m = fmaxf(m, sc.part_ml[slot(i) * kRows + r].x);
-#pragma unroll 8
-      for (int i = sub; i < np; i += kSub) {
-        const size_t row = slot(i) * kRows + r;
-        const float2 ml = sc.part_ml[row];
-        const float4 v = *reinterpret_cast<const float4*>(
-            sc.part_o + (kTiles ? ((slot(i) * (kRows / 128) + r / 128) * (D / 4) + c / 4) * 512 + (r % 128) * 4
-                                : row * D + c));
-        const float f = fast_exp2(ml.x - m);
-        if (ml.y != 0.f) {  // else nothing was visible there, and O may be unwritten
-          l = fmaf(f, ml.y, l);
-          o[0] = fmaf(f, v.x, o[0]);
-          o[1] = fmaf(f, v.y, o[1]);
-          o[2] = fmaf(f, v.z, o[2]);
-          o[3] = fmaf(f, v.w, o[3]);
+      // kAtOnce parts' loads in flight, then joined to what there is.
+      for (int i0 = sub; i0 < np; i0 += kAtOnce * kSub) {
+        float2 ml[kAtOnce];
+        float4 v[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+          const int i = i0 + k * kSub;
+          ml[k] = make_float2(kUnset, 0.f);
+          v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (i < np) {
+            const size_t row = slot(i) * kRows + r;
+            ml[k] = sc.part_ml[row];
+            v[k] = *reinterpret_cast<const float4*>(
+                sc.part_o +
+                (kTiles ? ((slot(i) * (kRows / 128) + r / 128) * (D / 4) + c / 4) * 512 + (r % 128) * 4
+                        : row * D + c));
+          }
+        }
+        float top = m;
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) top = fmaxf(top, ml[k].x);
+        const float f0 = fast_exp2(m - top);
+        m = top;
+        l *= f0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] *= f0;
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+          const float f = fast_exp2(ml[k].x - top);
+          l = fmaf(f, ml[k].y, l);
+          o[0] = fmaf(f, v[k].x, o[0]);
+          o[1] = fmaf(f, v[k].y, o[1]);
+          o[2] = fmaf(f, v[k].z, o[2]);
+          o[3] = fmaf(f, v[k].w, o[3]);
         }
       }
     }
@@ -126,7 +146,7 @@ cudaError_t launch_seq_join(const SeqAttnArgs& a, const SeqScratch& sc, bool til
   SeqScratch ss = sc;
   void* args[] = {&aa, &ss};
   prof_extra_launch();
-  return launch_pdl(table[a.d == 128][a.fp16 != 0][tiles], dim3(ctas, tiles ? 6 : 4), kThreads, 0, st, args);
+  return launch_pdl(table[a.d == 128][a.fp16 != 0][tiles], dim3(ctas, tiles ? 12 : 4), kThreads, 0, st, args);
 }
 
 }  // namespace vp

@@ -66,64 +66,61 @@ __device__ __forceinline__ void fill_place(const SeqAttnArgs& a, int b, Place* p
   p->n_rt = (int)(((long long)p->s.ql * a.group + kRows - 1) / kRows);
 }
 
-__device__ __forceinline__ long long seq_units(const SeqAttnArgs& a, int b) {
-  Place p;
-  fill_place(a, b, &p);
-  return p.units(a.Hkv);
+// Units per CTA.
+__device__ __forceinline__ long long units_per_cta(long long total, int P) {
+  return (total + P - 1) / P;
 }
 
-// Sum over the CTA (every thread gets it); scratch: 33 values.
-__device__ __forceinline__ long long cta_sum(long long v, long long* scratch) {
-#pragma unroll
-  for (int k = 16; k > 0; k >>= 1) v += __shfl_xor_sync(0xffffffffu, v, k);
-  __syncthreads();
-  if (lane_id() == 0) scratch[warp_id()] = v;
-  __syncthreads();
-  long long t = 0;
-  for (int w = 0; w < (int)blockDim.x / 32; ++w) t += scratch[w];
-  return t;
-}
-
-// The sequence that holds unit u < total, found by a scan of the lengths (all threads call it).
-__device__ __forceinline__ Place locate(const SeqAttnArgs& a, long long u, long long* scratch) {
-  const int n_warps = blockDim.x / 32, lane = lane_id(), w = warp_id();
-  long long before = 0;  // units before this round's sequences
-  __shared__ int s_b;
-  __shared__ long long s_base;
-  if (threadIdx.x == 0) {
-    s_b = 0;
-    s_base = 0;
+// The units of all sequences, and the place of this CTA's first one (if it has any): a scan of the
+// lengths by all threads, once where there are no more sequences than threads, else once for
+// the total and once for the place.  scratch: a value per warp.
+__device__ __forceinline__ long long find_place(const SeqAttnArgs& a, Place* place, long long* scratch) {
+  __shared__ Place s_place;
+  const int tid = threadIdx.x, n = blockDim.x, n_warps = n / 32, lane = lane_id(), w = warp_id();
+  if (tid == 0) {
+    s_place.b = 0;  // there always is one, but for sequences that change under the call
+    s_place.base = 0;
+    s_place.s = Seq{0, 0, 0};
+    s_place.n_kv = s_place.n_rt = 1;
   }
-  for (int b0 = 0; b0 < a.B; b0 += blockDim.x) {
-    const int b = b0 + threadIdx.x;
-    const long long mine = b < a.B ? seq_units(a, b) : 0;
-    long long v = mine;
+  long long all = 0;
+  for (int pass = a.B <= n ? 1 : 0; pass < 2; ++pass) {
+    long long before = 0;
+    for (int b0 = 0; b0 < a.B; b0 += n) {
+      Place p;
+      long long mine = 0;
+      if (b0 + tid < a.B) {
+        fill_place(a, b0 + tid, &p);
+        mine = p.units(a.Hkv);
+      }
+      long long v = mine;
 #pragma unroll
-    for (int k = 1; k < 32; k <<= 1) {
-      const long long x = __shfl_up_sync(0xffffffffu, v, k);
-      if (lane >= k) v += x;
+      for (int k = 1; k < 32; k <<= 1) {
+        const long long x = __shfl_up_sync(0xffffffffu, v, k);
+        if (lane >= k) v += x;
+      }
+      __syncthreads();
+      if (lane == 31) scratch[w] = v;
+      __syncthreads();
+      long long lead = before, total = before;
+      for (int i = 0; i < n_warps; ++i) {
+        if (i < w) lead += scratch[i];
+        total += scratch[i];
+      }
+      before = total;
+      if (pass == 0) continue;
+      if (a.B <= n) all = total;
+      const long long u = (long long)blockIdx.x * units_per_cta(all, gridDim.x), end = lead + v;
+      if (mine > 0 && end - mine <= u && u < end) {
+        p.base = end - mine;
+        s_place = p;
+      }
     }
-    __syncthreads();
-    if (lane == 31) scratch[w] = v;
-    __syncthreads();
-    long long lead = before, total = before;
-    for (int i = 0; i < n_warps; ++i) {
-      if (i < w) lead += scratch[i];
-      total += scratch[i];
-    }
-    const long long end = lead + v;
-    if (mine > 0 && end - mine <= u && u < end) {
-      s_b = b;
-      s_base = end - mine;
-    }
-    if (u < total) break;  // uniform
-    before = total;
+    if (pass == 0) all = before;
   }
   __syncthreads();
-  Place p;
-  fill_place(a, s_b, &p);
-  p.base = s_base;
-  return p;
+  *place = s_place;
+  return all;
 }
 
 // The next sequence with units.
@@ -138,9 +135,15 @@ __device__ __forceinline__ void advance(const SeqAttnArgs& a, Place* p) {
   p->base = base;
 }
 
-// Units per CTA.
-__device__ __forceinline__ long long units_per_cta(long long total, int P) {
-  return (total + P - 1) / P;
+// The segment at unit `rel` of a sequence: the item (kv head x row tile), and its key tile.
+__device__ __forceinline__ void segment_at(const Place& p, long long rel, int* item, int* tile) {
+  if (rel >> 32) {
+    *item = (int)(rel / p.n_kv);
+    *tile = (int)(rel - (long long)*item * p.n_kv);
+  } else {
+    *item = (uint32_t)rel / (uint32_t)p.n_kv;
+    *tile = (uint32_t)rel - *item * p.n_kv;
+  }
 }
 
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
@@ -218,14 +221,12 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
     tma_prefetch_desc(&tmap_v);
   }
   const int Hkv = prm.Hkv, group = prm.group, block = prm.block;
-  long long mine = 0;
-  for (int b = tid; b < prm.B; b += kThreads) mine += seq_units(prm, b);
-  const long long total = cta_sum(mine, scratch);  // its barriers also publish the mbarriers
+  Place pl;
+  const long long total = find_place(prm, &pl, scratch);  // its barriers also publish the mbarriers
   const long long per = units_per_cta(total, P);
   const long long begin = min(cta * per, total), end = min(begin + per, total);
   if (tid == 0) sc.recs[2 * cta] = make_int4(0, 0, 0, 0);  // until the producer knows better
   if (begin >= end) return;  // uniform
-  Place pl = locate(prm, begin, scratch);
   bool ok = true;
 
   if (warp == kWarps) {
@@ -235,7 +236,8 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
     const uint32_t box_bytes = (kPaged && ps < kBN ? ps : kBN) * 128;
     uint32_t lc = 0;
     for (long long u = begin; u < end && ok;) {
-      const int local = (int)((u - pl.base) % pl.n_kv), item = (int)((u - pl.base) / pl.n_kv);
+      int local, item;
+      segment_at(pl, u - pl.base, &item, &local);
       const int h = item / pl.n_rt, nk = (int)min((long long)(pl.n_kv - local), end - u);
       const int n_pages = kPaged ? (pl.s.kl + ps - 1) >> log2p : 0;
       const int32_t* table = kPaged ? prm.kv.table + (size_t)pl.b * prm.kv.width : nullptr;
@@ -302,8 +304,8 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
     const int v_key = lane & 15, v_chunk = lane >> 4;
     uint32_t lc = 0;
     for (long long u = begin; u < end && ok;) {
-      const long long rel = u - pl.base;
-      const int local = (int)(rel % pl.n_kv), item = (int)(rel / pl.n_kv);
+      int local, item;
+      segment_at(pl, u - pl.base, &item, &local);
       const int h = item / pl.n_rt, rt = item - h * pl.n_rt;
       const int nk = (int)min((long long)(pl.n_kv - local), end - u);
       const Seq s = pl.s;
