@@ -478,3 +478,83 @@ def test_chunks_through_the_cache_equal_the_whole_prompt():
     want = so.seq_attention(_f64(qr), _f64(kr), _f64(v), so.row_limits(L, L, 1), 0.125)
     _check_attention(_f64(torch.cat(parts)), None, want, BF, L, 6.0)
     _check_attention(_f64(whole), None, want, BF, L, 6.0)
+
+
+# ------------------------------------------------------------------------------ together
+def test_view_stream_example():
+    """The example's stack: views streamed through the cache against all views attended at once, and the
+    block's tokens against the 64-bit block."""
+    import examples.stream_views as ex
+
+    P, D, views = 70, 256, 5
+    g = torch.Generator(device="cuda").manual_seed(3)
+    blocks = [ex.make_block(g, D, 4, 2) for _ in range(2)]
+    x = torch.randn(views * P, D, generator=g, device="cuda").to(BF)
+    kw = dict(hq=4, hkv=2, block_tokens=P)
+    whole = ex.ViewStream(blocks, 1, views * P, **kw)
+    want = whole.extend(x, [views * P])
+    stream = ex.ViewStream(blocks, 2, views * P + 3, page_size=16, **kw)
+    got = [stream.extend(torch.cat((x[:2 * P], x[:P])), [2 * P, P])[:2 * P]]  # a second sequence beside it
+    got.append(stream.extend(x[2 * P:3 * P], [P, 0]))
+    got.append(stream.extend(torch.cat((x[3 * P:], x[P:2 * P])), [2 * P, P])[:2 * P])
+    got = torch.cat(got)
+    assert whole.errors() == 0 and stream.errors() == 0 and stream.held == [5 * P, 2 * P]
+    # Both sides round at the same points; where sums fall in another order a rounding may flip, and
+    # flips propagate through two blocks: a few bf16 steps of the residual stream at most.
+    d = (got.float() - want.float()).abs()
+    assert d.max() <= 4 * 2.0 ** -7 * want.float().abs().max() and d.mean() <= 2.0 ** -9 * want.float().abs().mean()
+    # a query is not kept
+    q = stream.query(x[:3], [2, 1])
+    assert q.shape == (3, D) and stream.held == [5 * P, 2 * P]
+    with pytest.raises(ValueError):
+        stream.extend(x[:4], [4, 0])
+    # one block in 64 bits
+    one = ex.ViewStream(blocks[:1], 1, views * P, **kw)
+    y = _f64(one.extend(x, [views * P]))
+    w = {k: _f64(v) for k, v in blocks[0].items()}
+    X = _f64(x)
+
+    def ln(t, gm, bt):
+        m, s = t.mean(-1, keepdims=True), t.var(-1, keepdims=True)
+        return (t - m) / np.sqrt(s + 1e-6) * gm + bt
+
+    qkv = (ln(X, w["ln1_g"], w["ln1_b"]) @ w["w_qkv"].T + w["b_qkv"]).reshape(-1, 8, 64)
+    ang = so.rope_angles(np.arange(views * P), 10000.0 ** (-2.0 * np.arange(32) / 64))
+    o = so.seq_attention(so.rope(qkv[:, :4], ang), so.rope(qkv[:, 4:6], ang), qkv[:, 6:],
+                         so.row_limits(views * P, views * P, P), 0.125)[0]
+    X = X + w["ls1"] * (o.reshape(-1, 256) @ w["w_o"].T + w["b_o"])
+    h = ln(X, w["ln2_g"], w["ln2_b"]) @ w["w_fc1"].T + w["b_fc1"]
+    h = 0.5 * h * (1 + np.vectorize(math.erf)(h / math.sqrt(2)))
+    X = X + w["ls2"] * (h @ w["w_fc2"].T + w["b_fc2"])
+    err = np.abs(y - X)
+    # about ten bf16 roundings on the way (QKV, rotation, P, Y, LN2, hidden, two residual sums)
+    assert err.max() <= 10 * 2.0 ** -8 * np.abs(X).max() and err.mean() <= 2.0 ** -7 * np.abs(X).mean()
+
+
+def test_calls_in_a_graph_follow_their_inputs():
+    """A captured step replayed after its inputs changed (lengths, tokens, pages) computes on the new ones."""
+    dims = vpb.attn_dims(8, 2, 64)
+    c = Cache(11, [700, 90], 2, 64, 32, BF)
+    k = _randn(5, 2, 2, 64, dtype=BF)
+    q, out = _randn(6, 2, 8, 64, dtype=BF), torch.empty(2, 8, 64, dtype=BF, device="cuda")
+    qr = torch.empty_like(q)
+    cu, ws = _cu([1, 1]), _dirty_ws(dims, 2, 2)
+    rope = vpb.rope_options(vpb.rope_turns(64).cuda())
+    kv_len = c.kv_len.clone()
+
+    def step():
+        vpb.vp_rope_append(dims, rope, q, k, k, cu, kv_len, None, c.kv, q_out=qr)
+        vpb.vp_paged_attention(dims, qr, cu, kv_len, c.kv, out, None, ws)
+
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for lens in ([700, 90], [650, 33], [1, 64]):
+        kv_len.copy_(torch.tensor(lens, dtype=torch.int32))
+        q.copy_(_randn(60 + lens[0], 2, 8, 64, dtype=BF))
+        graph.replay()
+        got = out.clone()
+        out.zero_()
+        step()
+        assert torch.equal(got, out)
