@@ -459,25 +459,22 @@ def attn_workspace(dims: VpAttnDims, T: int, B: int, device="cuda") -> torch.Ten
     return ws
 
 
-def _rows_p(t, heads, dims, T=None):
-    """(address, token stride) of a [T][heads][d] tensor whose heads and channels are contiguous."""
+_TORCH_DTYPES = {v: k for k, v in VP_DTYPES.items()}
+
+
+def _rows_p(t, shape, dtype):
+    """(address, token stride) of a [T][heads][d] device tensor whose heads and channels are contiguous."""
     if t is None:
         return None, 0
-    d = dims.d
-    if t.dim() != 3:
-        raise ValueError(f"expected three dimensions, got {list(t.shape)}")
-    n, h, c = t.shape
-    if h != heads or c != d or (T is not None and n != T):
-        raise ValueError(f"expected [{'T' if T is None else T}][{heads}][{d}], got {list(t.shape)}")
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda:
+        raise ValueError(f"expected a device tensor {list(shape)} of {dtype}, got {list(t.shape)} of {t.dtype} on "
+                         f"{t.device}")
+    T, heads, d = shape
     s0, s1, s2 = t.stride()
     if s2 != 1 or (s1 != d and heads > 1):
         raise ValueError("heads and channels must be contiguous")
-    if VP_DTYPES.get(t.dtype, -1) != dims.dtype:
-        raise ValueError(f"the tensor's type {t.dtype} is not that of dims")
-    if not t.is_cuda:
-        raise ValueError("device tensors are required (the library has no CPU path)")
     # a single token has no stride of its own: any legal one stands for it
-    return t.data_ptr(), s0 if n > 1 else heads * d
+    return t.data_ptr(), s0 if T > 1 else heads * d
 
 
 def _ints_p(t, n, what):
@@ -501,12 +498,13 @@ def _kv_ref(kv, dims, B):
 def vp_rope_append(dims: VpAttnDims, rope: VpRopeOptions, q, k, v, cu, kv_len, positions, kv: VpPagedKv = None,
                    q_out=None, k_out=None, ws=None, stream=None):
     """Rotates q into q_out and k into the cache (and / or k_out), and writes v to the cache."""
-    T, B = k.shape[0], cu.numel() - 1
-    qp, qs = _rows_p(q, dims.Hq, dims, T)
-    kp, ks = _rows_p(k, dims.Hkv, dims, T)
-    vp, vs = _rows_p(v, dims.Hkv, dims, T)
-    qo, qos = _rows_p(q_out, dims.Hq, dims, T)
-    ko, kos = _rows_p(k_out, dims.Hkv, dims, T)
+    T, B, d, dt = k.shape[0], cu.numel() - 1, dims.d, _TORCH_DTYPES.get(dims.dtype)
+    q_shape, kv_shape = (T, dims.Hq, d), (T, dims.Hkv, d)
+    qp, qs = _rows_p(q, q_shape, dt)
+    kp, ks = _rows_p(k, kv_shape, dt)
+    vp, vs = _rows_p(v, kv_shape, dt)
+    qo, qos = _rows_p(q_out, q_shape, dt)
+    ko, kos = _rows_p(k_out, kv_shape, dt)
     _check(lib().vp_rope_append(ctypes.byref(dims), ctypes.byref(rope), T, B, qp, qs, kp, ks, vp, vs,
                                 _ints_p(cu, B + 1, "cu"), _ints_p(kv_len, B, "kv_len"),
                                 _ints_p(positions, T, "positions"), _kv_ref(kv, dims, B), qo, qos, ko, kos, _p(ws),
@@ -528,11 +526,12 @@ def _lse_p(lse, T, dims):
 
 
 def vp_prompt_attention(dims: VpAttnDims, q, k, v, cu, out, lse, ws, stream=None):
-    T, B = q.shape[0], cu.numel() - 1
-    qp, qs = _rows_p(q, dims.Hq, dims)
-    kp, ks = _rows_p(k, dims.Hkv, dims, T)
-    vp, vs = _rows_p(v, dims.Hkv, dims, T)
-    op, os_ = _rows_p(out, dims.Hq, dims, T)
+    T, B, d, dt = q.shape[0], cu.numel() - 1, dims.d, _TORCH_DTYPES.get(dims.dtype)
+    q_shape, kv_shape = (T, dims.Hq, d), (T, dims.Hkv, d)
+    qp, qs = _rows_p(q, q_shape, dt)
+    kp, ks = _rows_p(k, kv_shape, dt)
+    vp, vs = _rows_p(v, kv_shape, dt)
+    op, os_ = _rows_p(out, q_shape, dt)
     _check(lib().vp_prompt_attention(ctypes.byref(dims), T, B, qp, qs, kp, ks, vp, vs, _ints_p(cu, B + 1, "cu"), op,
                                      os_, _lse_p(lse, T, dims), *_ws_p(ws), _stream(stream)),
            "vp_prompt_attention")
@@ -540,8 +539,9 @@ def vp_prompt_attention(dims: VpAttnDims, q, k, v, cu, out, lse, ws, stream=None
 
 def vp_paged_attention(dims: VpAttnDims, q, cu, kv_len, kv: VpPagedKv, out, lse, ws, stream=None):
     T, B = q.shape[0], cu.numel() - 1
-    qp, qs = _rows_p(q, dims.Hq, dims)
-    op, os_ = _rows_p(out, dims.Hq, dims, T)
+    shape, dt = (T, dims.Hq, dims.d), _TORCH_DTYPES.get(dims.dtype)
+    qp, qs = _rows_p(q, shape, dt)
+    op, os_ = _rows_p(out, shape, dt)
     _check(lib().vp_paged_attention(ctypes.byref(dims), T, B, qp, qs, _ints_p(cu, B + 1, "cu"),
                                     _ints_p(kv_len, B, "kv_len"), _kv_ref(kv, dims, B), op, os_,
                                     _lse_p(lse, T, dims), *_ws_p(ws), _stream(stream)), "vp_paged_attention")

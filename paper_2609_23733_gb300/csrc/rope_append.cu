@@ -35,10 +35,13 @@ __device__ __forceinline__ uint32_t rotate_adjacent(uint32_t u, float2 cs) {
 }
 
 template <bool F16>
-__global__ void __launch_bounds__(kRaThreads) rope_append_kernel(RopeAppendArgs a, int tokens) {
+__global__ void __launch_bounds__(kRaThreads) rope_append_kernel(const __grid_constant__ RopeAppendArgs a,
+                                                               int tokens) {
   __shared__ float2 s_cs[kRaTokens * 64];
   __shared__ long long s_row[kRaTokens];  // row (of d channels) of kv head 0 in the cache, -1: none
   __shared__ int s_pos[kRaTokens];
+  pdl_launch_dependents();
+  pdl_wait();
   const int t0 = blockIdx.x * tokens;
   const int nt = min(min(tokens, a.T - t0), a.cu[a.B] - t0);
   if (nt <= 0) return;  // uniform
@@ -156,13 +159,14 @@ cudaError_t launch_rope_append(const RopeAppendArgs& a, int num_sms, cudaStream_
   int tokens = a.T / (4 * num_sms);
   tokens = tokens < 1 ? 1 : tokens > kRaTokens ? kRaTokens : tokens;
   const int grid = (a.T + tokens - 1) / tokens;
+  RopeAppendArgs aa = a;
+  void* args[] = {&aa, &tokens};
+  const void* fn = a.fp16 ? reinterpret_cast<const void*>(rope_append_kernel<true>)
+                          : reinterpret_cast<const void*>(rope_append_kernel<false>);
   prof_before(VP_KERNEL_ROPE_APPEND, st);
-  if (a.fp16)
-    rope_append_kernel<true><<<grid, kRaThreads, 0, st>>>(a, tokens);
-  else
-    rope_append_kernel<false><<<grid, kRaThreads, 0, st>>>(a, tokens);
+  const cudaError_t e = launch_pdl(fn, dim3(grid), kRaThreads, 0, st, args);
   prof_after(st);
-  return cudaGetLastError();
+  return e;
 }
 
 }  // namespace vp

@@ -435,8 +435,6 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
   volatile int* abort_flag = &sm.abort_flag;
   unsigned int* err = prm.err;
   pdl_launch_dependents();
-  find_run<C>(prm, sc, reinterpret_cast<int4*>(sm.q), &sm.run);
-  fence_proxy_async_smem();  // sm.q was scratch: before the copies into it
 
   if (threadIdx.x == 0) {
     for (int c = 0; c < kChains; ++c) {
@@ -470,6 +468,9 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
     tmem_alloc(&sm.tmem_base, 512);
     tmem_relinquish();
   }
+  pdl_wait();  // what is ahead in the stream: the inputs are there, and the last call's join is over
+  find_run<C>(prm, sc, reinterpret_cast<int4*>(sm.q), &sm.run);
+  fence_proxy_async_smem();  // sm.q was scratch: before the copies into it
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -1039,8 +1040,10 @@ cudaError_t launch_tiles(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms
   const void* tile = reinterpret_cast<const void*>(seq_tile_kernel<D, F16, kPaged>);
   e = cudaFuncSetAttribute(tile, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  seq_tile_kernel<D, F16, kPaged><<<P, C::kThreads, smem, st>>>(mq, mk, mv, a, sc);
-  e = cudaGetLastError();
+  SeqAttnArgs aa = a;
+  SeqScratch ss = sc;
+  void* args[] = {&mq, &mk, &mv, &aa, &ss};
+  e = launch_pdl(tile, dim3(P), C::kThreads, smem, st, args);
   // Items of at most kItemCost + 7 key tiles are never cut (find_run): nothing to join.
   const long long keys = kPaged ? (long long)a.kv.width << a.kv.log2_page : a.T;
   if (e != cudaSuccess || keys <= (C::kItemCost + 7) * C::kBN) return e;

@@ -26,6 +26,7 @@ __global__ void __launch_bounds__(kThreads)
   constexpr int kRows = kTiles ? seq_chains(D) * 128 : kSmallRows;  // rows of a slot
   __shared__ __align__(16) float s_o[kTiles ? 1 : kThreads][4];
   __shared__ __align__(8) float2 s_ml[kTiles ? 1 : kThreads];
+  pdl_launch_dependents();
   pdl_wait();
   const int cta = blockIdx.x;
   const int4 x = sc.recs[2 * cta], y = sc.recs[2 * cta + 1];

@@ -221,6 +221,7 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
     tma_prefetch_desc(&tmap_v);
   }
   const int Hkv = prm.Hkv, group = prm.group, block = prm.block;
+  pdl_wait();  // what is ahead in the stream: the inputs are there, and the last call's join is over
   Place pl;
   const long long total = find_place(prm, &pl, scratch);  // its barriers also publish the mbarriers
   const long long per = units_per_cta(total, P);
@@ -547,8 +548,10 @@ cudaError_t launch_rows(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms,
   const void* fn = reinterpret_cast<const void*>(seq_rows_kernel<D, F16, kPaged>);
   e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  seq_rows_kernel<D, F16, kPaged><<<P, kThreads, smem, st>>>(mk, mv, a, sc);
-  e = cudaGetLastError();
+  SeqAttnArgs aa = a;
+  SeqScratch ss = sc;
+  void* args[] = {&mk, &mv, &aa, &ss};
+  e = launch_pdl(fn, dim3(P), kThreads, smem, st, args);
   if (e != cudaSuccess) return e;
   const long long keys = kPaged ? (long long)a.kv.width << a.kv.log2_page : a.T;
   if (keys <= kBN) return e;  // items of one unit: nothing is cut

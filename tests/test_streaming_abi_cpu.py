@@ -167,7 +167,6 @@ def test_struct_layouts():
 
 
 def test_binding_refuses_before_the_library():
-    dims = vpb.attn_dims(4, 2, 64)
     with pytest.raises(ValueError):
         vpb.attn_dims(4, 2, 64, dtype=torch.float32)
     z = torch.zeros
@@ -184,7 +183,7 @@ def test_binding_refuses_before_the_library():
                 z(5, 64, 4, dtype=b).transpose(1, 2), z(5, 8, 64, dtype=b)[:, ::2], z(5, 4, 64, dtype=torch.float16),
                 z(5, 4, 64, dtype=b)):  # (the last: right but for living on the CPU)
         with pytest.raises(ValueError):
-            vpb._rows_p(bad, 4, dims)
+            vpb._rows_p(bad, (5, 4, 64), b)
     for bad in (z(3, dtype=torch.int64), z(4, dtype=torch.int32), z(3, dtype=torch.int32)):
         with pytest.raises(ValueError):
             vpb._ints_p(bad, 3, "cu")
