@@ -374,7 +374,7 @@ __device__ __forceinline__ void find_run(const SeqAttnArgs& a, const SeqScratch&
   const int P = gridDim.x, cta = blockIdx.x;
   long long per = 0, near = 0, x0 = 0, x1 = 0;
   auto on_total = [&](long long total) {
-    per = (total + P - 1) / P;
+    per = (total + P - 1) >> 32 ? (total + P - 1) / P : (long long)((uint32_t)(total + P - 1) / (uint32_t)P);
     near = max(per / 128, kItemCost + 4ll);
     x0 = cta * per;
     x1 = x0 + per;
@@ -535,7 +535,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       }
       for (int jj = 0; jj < it.nk; ++jj, ++lc) {
         const int j = it.j0 + jj, st = lc % kStages;
-        int y = it.q0 + j * kBN, page = 0, n_box = 1;
+        int y = it.q0 + j * kBN, at = 0, n_box = 1;
         if (kPaged) {
           const int p0 = (j * kBN) >> log2p;
           if (p0 >= first + 32) {
@@ -544,41 +544,43 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
             next = first + 32 + lane < n_pages ? table[first + 32 + lane] : 0;
           }
           n_box = min(ppt, n_pages - p0);  // the pages that exist; the rest of the tile is masked
-          page = __shfl_sync(0xffffffffu, window, (p0 - first + lane) & 31);
+          at = p0 - first;
           y = (j * kBN) & (ps - 1);
-          if (lane < n_box && (unsigned)page >= (unsigned)prm.kv.n_pages) atomicOr(err, VP_DEVERR_PAGE);
         }
-        const uint32_t par = ((lc / kStages) & 1) ^ 1;
-        const int off = lane * (box_bytes / 2);
-        if (kAlias) {
-          ok = mbar_wait_warp(&sm.k_empty[st], par, err, abort_flag);
-        } else {  // K and V of a tile are released together
-          ok = mbar_wait_warp(&sm.v_empty[st], par, err, abort_flag);
-        }
+        const uint32_t par = ((lc / kStages) & 1) ^ 1, bytes = n_box * kHalves * box_bytes;
+        // Page after page by one elected lane, with coordinates that are the same on all lanes.
+        auto copy = [&](uint16_t (*dst)[kBN * 64], const CUtensorMap* map, uint64_t* bar) {
+          for (int i = 0; i < n_box; ++i) {
+            const int page = kPaged ? __shfl_sync(0xffffffffu, window, at + i) : 0;
+            if (kPaged && (unsigned)page >= (unsigned)prm.kv.n_pages && lane == 0)
+              atomicOr(err, VP_DEVERR_PAGE);
+            if (elect_one()) {
+#pragma unroll
+              for (int hf = 0; hf < kHalves; ++hf)
+                tma_load_4d(dst[hf] + i * (box_bytes / 2), map, bar, hf * 64, y, it.h, page);
+            }
+            __syncwarp();
+          }
+        };
+        // K and V of a tile are released apart with 128-key tiles, together with 64-key ones.
+        ok = mbar_wait_warp(kAlias ? &sm.k_empty[st] : &sm.v_empty[st], par, err, abort_flag);
         if (!ok) break;
-        if (lane == 0) {
-          mbar_arrive_expect_tx(&sm.k_full[st], n_box * kHalves * box_bytes);
-          if (!kAlias) mbar_arrive_expect_tx(&sm.v_full[st], n_box * kHalves * box_bytes);
+        if (elect_one()) {
+          mbar_arrive_expect_tx(&sm.k_full[st], bytes);
+          if (!kAlias) mbar_arrive_expect_tx(&sm.v_full[st], bytes);
         }
         __syncwarp();
-        if (lane < n_box)
-#pragma unroll
-          for (int hf = 0; hf < kHalves; ++hf)
-            tma_load_4d(sm.k[st][hf] + off, &tmap_k, &sm.k_full[st], hf * 64, y, it.h, page);
+        copy(sm.k[st], &tmap_k, &sm.k_full[st]);
         if (kAlias) {
           ok = mbar_wait_warp(&sm.v_empty[st], par, err, abort_flag);
           if (!ok) {
             k_ahead = 1;
             break;
           }
-          if (lane == 0) mbar_arrive_expect_tx(&sm.v_full[st], n_box * kHalves * box_bytes);
+          if (elect_one()) mbar_arrive_expect_tx(&sm.v_full[st], bytes);
           __syncwarp();
         }
-        if (lane < n_box)
-#pragma unroll
-          for (int hf = 0; hf < kHalves; ++hf)
-            tma_load_4d(sm.v[st][hf] + off, &tmap_v, &sm.v_full[st], hf * 64, y, it.h, page);
-        __syncwarp();
+        copy(sm.v[st], &tmap_v, &sm.v_full[st]);
         if (jj == 0) {  // the other chains' Q behind the first keys
           load_q(1, kChains);
           if (!ok) {

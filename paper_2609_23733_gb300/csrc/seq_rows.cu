@@ -6,9 +6,9 @@
 // mma.sync m16n8k16 with the rows padded to 16 keeps up with HBM and needs no TMEM round
 // trip per tile.  What counts is bytes in flight on every SM and an even cut of the work.
 //
-// The work is the sequence of units (sequence, kv head, 16 rows, 64 keys); CTA c of P takes
-// the units [c u, (c + 1) u), whatever items they belong to, so that all CTAs end together
-// for any mix of lengths; an item (16 rows of a kv head) that a CTA holds in part leaves a
+// The work is the sequence of units (sequence, kv head, 16 rows, 64 keys), an item's (16 rows of a
+// kv head) with kItemCost added; CTA c of P takes the c-th of P equal runs, whatever items they
+// belong to, so that all CTAs end together for any mix of lengths; an item (16 rows of a kv head) that a CTA holds in part leaves a
 // partial result, and seq_join_kernel (a programmatic dependent launch) joins the parts in order.  Each CTA finds its place by a scan over the sequences' lengths.
 //   warp 4      TMA: K / V tiles through a ring, page by page (page ids read 32 ahead).
 //   warps 0-3   16 keys of every tile each: S = Q K^T (16 x 16), softmax against the warp's own
@@ -31,6 +31,12 @@ constexpr int kWarps = 4;          // compute warps
 constexpr int kThreads = 32 * (kWarps + 1);
 constexpr float kUnset = -1e30f;
 constexpr float kRescaleThreshold = 8.f;  // log2 units
+// An item costs about as much as this many units on top of its own (its rows' q, the join of the warps):
+// the extent of an item is kItemCost + its units, and cuts within the first kItemCost move to its start.
+#ifndef VP_ROWS_ITEM_COST
+#define VP_ROWS_ITEM_COST 4
+#endif
+constexpr int kItemCost = VP_ROWS_ITEM_COST;
 
 template <int D>
 struct RowsCfg {
@@ -50,13 +56,14 @@ struct RowsSmem {
   int abort_flag;
 };
 
-// A sequence's place in the order of units.
+// A sequence's place in the order of items.
 struct Place {
   int b;             // a.B: past the end
-  long long base;    // units before it
+  long long base;    // the extent of all items before it
   Seq s;
   int n_kv, n_rt;    // key tiles, 16-row tiles per kv head
-  __device__ __forceinline__ long long units(int Hkv) const { return (long long)Hkv * n_rt * n_kv; }
+  __device__ __forceinline__ int item() const { return n_kv + kItemCost; }
+  __device__ __forceinline__ long long extent(int Hkv) const { return (long long)Hkv * n_rt * item(); }
 };
 
 __device__ __forceinline__ void fill_place(const SeqAttnArgs& a, int b, Place* p) {
@@ -68,7 +75,8 @@ __device__ __forceinline__ void fill_place(const SeqAttnArgs& a, int b, Place* p
 
 // Units per CTA.
 __device__ __forceinline__ long long units_per_cta(long long total, int P) {
-  return (total + P - 1) / P;
+  const long long x = total + P - 1;
+  return x >> 32 ? x / P : (long long)((uint32_t)x / (uint32_t)P);
 }
 
 // The units of all sequences, and the place of this CTA's first one (if it has any): a scan of the
@@ -91,7 +99,7 @@ __device__ __forceinline__ long long find_place(const SeqAttnArgs& a, Place* pla
       long long mine = 0;
       if (b0 + tid < a.B) {
         fill_place(a, b0 + tid, &p);
-        mine = p.units(a.Hkv);
+        mine = p.extent(a.Hkv);
       }
       long long v = mine;
 #pragma unroll
@@ -123,27 +131,40 @@ __device__ __forceinline__ long long find_place(const SeqAttnArgs& a, Place* pla
   return all;
 }
 
-// The next sequence with units.
+// The next sequence with items.
 __device__ __forceinline__ void advance(const SeqAttnArgs& a, Place* p) {
-  long long base = p->base + p->units(a.Hkv);
+  long long base = p->base + p->extent(a.Hkv);
   int b = p->b + 1;
   for (; b < a.B; ++b) {
     fill_place(a, b, p);
-    if (p->units(a.Hkv) > 0) break;
+    if (p->extent(a.Hkv) > 0) break;
   }
   p->b = b;
   p->base = base;
 }
 
-// The segment at unit `rel` of a sequence: the item (kv head x row tile), and its key tile.
-__device__ __forceinline__ void segment_at(const Place& p, long long rel, int* item, int* tile) {
-  if (rel >> 32) {
-    *item = (int)(rel / p.n_kv);
-    *tile = (int)(rel - (long long)*item * p.n_kv);
-  } else {
-    *item = (uint32_t)rel / (uint32_t)p.n_kv;
-    *tile = (uint32_t)rel - *item * p.n_kv;
-  }
+// What a CTA's run [begin, end) holds of one item.
+struct Segment {
+  int h, rt;        // kv head, row tile
+  int t0, t1;       // key tiles
+  bool part;        // not all of the item's
+  long long item0;  // where the item begins
+};
+
+// The segment at u; false if the run holds none of the item (a cut within its first kItemCost).
+__device__ __forceinline__ bool segment_at(const Place& p, long long u, long long end, Segment* s) {
+  const long long rel = u - p.base;
+  const int ext = p.item();
+  const int item = rel >> 32 ? (int)(rel / ext) : (int)((uint32_t)rel / (uint32_t)ext);
+  s->item0 = p.base + (long long)item * ext;
+  const int from = (int)(u - s->item0), to = (int)min((long long)ext, end - s->item0);
+  if (to < ext && to <= kItemCost) return false;
+  s->h = item / p.n_rt;
+  s->rt = item - s->h * p.n_rt;
+  s->t0 = max(from - kItemCost, 0);
+  s->t1 = to - kItemCost;
+  s->part = s->t0 > 0 || s->t1 < p.n_kv;
+  return true;
 }
 
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
@@ -237,19 +258,19 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
     const uint32_t box_bytes = (kPaged && ps < kBN ? ps : kBN) * 128;
     uint32_t lc = 0;
     for (long long u = begin; u < end && ok;) {
-      int local, item;
-      segment_at(pl, u - pl.base, &item, &local);
-      const int h = item / pl.n_rt, nk = (int)min((long long)(pl.n_kv - local), end - u);
+      Segment sg;
+      if (!segment_at(pl, u, end, &sg)) break;
+      const int h = sg.h;
       const int n_pages = kPaged ? (pl.s.kl + ps - 1) >> log2p : 0;
       const int32_t* table = kPaged ? prm.kv.table + (size_t)pl.b * prm.kv.width : nullptr;
-      int first = kPaged ? (local * kBN) >> log2p : 0, window = 0, next = 0;
+      int first = kPaged ? (sg.t0 * kBN) >> log2p : 0, window = 0, next = 0;
       if (kPaged) {
         if (first + lane < n_pages) window = table[first + lane];
         if (first + 32 + lane < n_pages) next = table[first + 32 + lane];
       }
-      for (int j = local; j < local + nk; ++j, ++lc) {
+      for (int j = sg.t0; j < sg.t1; ++j, ++lc) {
         const int st = lc % kStages;
-        int y = pl.s.q0 + j * kBN, page = 0, n_box = 1;
+        int y = pl.s.q0 + j * kBN, at = 0, n_box = 1;
         if (kPaged) {
           const int p0 = (j * kBN) >> log2p;
           if (p0 >= first + 32) {
@@ -258,34 +279,38 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
             next = first + 32 + lane < n_pages ? table[first + 32 + lane] : 0;
           }
           n_box = min(ppt, n_pages - p0);  // the pages that exist; the rest of the tile is masked
-          page = __shfl_sync(0xffffffffu, window, (p0 - first + lane) & 31);
+          at = p0 - first;
           y = (j * kBN) & (ps - 1);
-          if (lane < n_box && (unsigned)page >= (unsigned)prm.kv.n_pages) atomicOr(err, VP_DEVERR_PAGE);
         }
         ok = mbar_wait_warp(&sm.empty[st], ((lc / kStages) & 1) ^ 1, err, abort_flag);
         if (!ok) break;
-        if (lane == 0) mbar_arrive_expect_tx(&sm.full[st], 2 * n_box * kHalves * box_bytes);
+        if (elect_one()) mbar_arrive_expect_tx(&sm.full[st], 2 * n_box * kHalves * box_bytes);
         __syncwarp();
-        if (lane < n_box) {
-          const int off = lane * (box_bytes / 2);
+        // One elected lane copies page after page: coordinates that differ between lanes would cost
+        // the copies' issue 800 clocks a tile, more than twice as much.
+        for (int i = 0; i < n_box; ++i) {
+          const int page = kPaged ? __shfl_sync(0xffffffffu, window, at + i) : 0;
+          if (kPaged && (unsigned)page >= (unsigned)prm.kv.n_pages && lane == 0) atomicOr(err, VP_DEVERR_PAGE);
+          const int off = i * (box_bytes / 2);
+          if (elect_one()) {
 #pragma unroll
-          for (int hf = 0; hf < kHalves; ++hf) {
-            tma_load_4d(sm.k[st][hf] + off, &tmap_k, &sm.full[st], hf * 64, y, h, page);
-            tma_load_4d(sm.v[st][hf] + off, &tmap_v, &sm.full[st], hf * 64, y, h, page);
+            for (int hf = 0; hf < kHalves; ++hf) {
+              tma_load_4d(sm.k[st][hf] + off, &tmap_k, &sm.full[st], hf * 64, y, h, page);
+              tma_load_4d(sm.v[st][hf] + off, &tmap_v, &sm.full[st], hf * 64, y, h, page);
+            }
           }
+          __syncwarp();
         }
-        __syncwarp();
       }
-      // This CTA's entry of the list of cut items: one whose first part ends this run.
-      if (u + nk == end && lane == 0) {
-        const long long item0 = u - local, item1 = item0 + pl.n_kv;
-        const bool cut = end < item1 && item0 >= begin;
-        const int np = cut ? (int)((item1 - 1) / per) - cta + 1 : 0;
-        sc.recs[2 * cta] = make_int4(np, h, item - h * pl.n_rt, pl.b);
-        sc.recs[2 * cta + 1] = make_int4(pl.s.q0, pl.s.ql, pl.s.kl, 2 * cta + (item0 > begin));
+      // This CTA's entry of the list of cut items: one whose first part ends this run.  The cuts k per
+      // of the item that stay: item0 + kItemCost < k per < item0 + its extent.
+      if (sg.t1 < pl.n_kv && sg.t0 == 0 && lane == 0) {
+        const int last = (int)((sg.item0 + pl.item() - 1) / per);
+        sc.recs[2 * cta] = make_int4(last - cta + 1, h, sg.rt, pl.b);
+        sc.recs[2 * cta + 1] = make_int4(pl.s.q0, pl.s.ql, pl.s.kl, 2 * cta + (u > begin));
       }
-      u += nk;
-      if (u < end && u - pl.base >= pl.units(Hkv)) advance(prm, &pl);
+      u = sg.item0 + pl.item();
+      if (u < end && u - pl.base >= pl.extent(Hkv)) advance(prm, &pl);
     }
     // The copies land before the CTA releases its shared memory (after a timeout nobody else
     // may be waiting for them).
@@ -305,10 +330,9 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
     const int v_key = lane & 15, v_chunk = lane >> 4;
     uint32_t lc = 0;
     for (long long u = begin; u < end && ok;) {
-      int local, item;
-      segment_at(pl, u - pl.base, &item, &local);
-      const int h = item / pl.n_rt, rt = item - h * pl.n_rt;
-      const int nk = (int)min((long long)(pl.n_kv - local), end - u);
+      Segment sg;
+      if (!segment_at(pl, u, end, &sg)) break;
+      const int h = sg.h, rt = sg.rt;
       const Seq s = pl.s;
       int tok[2], head[2], lim[2];
       bool valid[2];
@@ -334,7 +358,7 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[n][i] = 0.f;
 
-      for (int j = local; j < local + nk; ++j, ++lc) {
+      for (int j = sg.t0; j < sg.t1; ++j, ++lc) {
         const int st = lc % kStages;
         ok = mbar_wait_warp(&sm.full[st], (lc / kStages) & 1, err, abort_flag);
         if (!ok) break;
@@ -504,7 +528,7 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
         if (warp == 0) add(sm.o[1]);
       }
       if (warp == 0) {
-        if (local == 0 && nk == pl.n_kv) {  // the whole item
+        if (!sg.part) {  // the whole item
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             if (!valid[i]) continue;
@@ -531,8 +555,8 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
           }
         }
       }
-      u += nk;
-      if (u < end && u - pl.base >= pl.units(Hkv)) advance(prm, &pl);
+      u = sg.item0 + pl.item();
+      if (u < end && u - pl.base >= pl.extent(Hkv)) advance(prm, &pl);
     }
   }
 }
