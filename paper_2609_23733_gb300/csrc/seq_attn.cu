@@ -2,22 +2,27 @@
 // cache (vp_paged_attention), on the sm_103a tensor cores: o = sum_j p_j v_j / sum_j p_j over the
 // keys j < lim(i) that row (token i, head h) sees, p_j = 2^(s_j - m), s_j = scale log2(e) q . k_j.
 //
-// Work.  A tile is kChains x (128 / group) tokens of a sequence with all heads of one kv head's group
-// (row = token x group + head, so K and V are read once for the group).  The work is the
-// sequence of units (tile, kv head, 64 keys that the tile's last row sees); CTA c of P (one per SM)
-// takes an equal run of them, whatever items (tile, kv head) they belong to, so that all CTAs end
-// together for any mix of lengths (a cut within a 128th of a share from an item's end moves
-// there).  Each CTA finds its run by a scan of the lengths.  An item that a CTA holds
-// in part leaves its unnormalised output; seq_join_kernel (a programmatic dependent launch)
-// joins the parts in order.  Against whole items in descending order with long ones halved (a
-// list written by a kernel ahead): see the figures at launch_tiles.
+// Work.  A tile is kChains chains of 128 / group tokens of a sequence with all heads of one kv head's
+// group (row = token x group + head, so K and V are read once for the group).  The work is the
+// sequence of units (tile, kv head, kBN keys that the tile's last row sees), an item's (tile, kv
+// head) with kItemCost added for its start and end; CTA c of P (one per SM) takes the c-th of P
+// equal runs, whatever items they belong to, so that all CTAs end together for any mix of
+// lengths (a cut very near an item's end moves there).  Each CTA finds its run by a scan of the
+// lengths.  An item that a CTA holds in part leaves its unnormalised output, and seq_join_kernel
+// (a programmatic dependent launch) joins the parts in order.  A list of whole items in descending
+// order, the long ones halved, was 1.4 to 1.6 times slower for chunks over a cache (few,
+// long items: 374 against 229 us for 1,374 tokens over 43,968 keys) and needed a kernel ahead.
 //
-// The tile kernel.  The kChains 128-row tiles of an item run as independent chains that share the
-// K / V ring (64 keys per tile): the tensor core works for one chain while another's softmax runs.
+// The tile kernel.  The chains (128 rows each) of an item share the K / V ring; the tensor core works
+// for one chain while another's softmax runs.  d 64: three chains, 64-key tiles, S, P and O of a
+// chain in TMEM columns of their own, S of the next tile issued as soon as S has been read.  d 128:
+// two chains, 128-key tiles (S at the full rate with both operands in shared memory; 64-key tiles,
+// whose S runs at two thirds of it, measured 1,400 against 1,550 TFLOP/s), P in the first
+// columns of S, the chains' products issued by turns.
 //   warp 0               TMA: Q once per item; K / V tiles, page by page, page ids read a window of
-//                        32 ahead by the lanes.
-//   warps 1 .. kChains   one elected lane issues a chain's tcgen05.mma: S = Q K^T (128 x 64, fp32 in
-//                        TMEM), O += P V (P read from TMEM as 16-bit pairs).
+//                        32 ahead by the lanes; it walks the run and publishes the items.
+//   warps 1 .. kChains   one elected lane issues a chain's tcgen05.mma: S = Q K^T (fp32 in TMEM),
+//                        O += P V (P read from TMEM as 16-bit pairs).
 //   warps 4 ..           four softmax warps per chain, a row per thread; the running maximum
 //                        is moved only when it grows by more than 2^8 (exact either way).
 // A chain stops at its own last visible key; the tiles after it are only released.  A tile that
@@ -27,7 +32,14 @@
 // them added back in the epilogue (a flag says whether there were any), those of the other
 // chains too: adding an infinity or a NaN to a sum that has it already changes nothing.
 // Scores, maxima, sums and outputs are held in 32 bits; P is rounded to the storage type, as the
-// tensor core needs.  Every wait is bounded; a CTA that gives up lets its copies and MMAs land.
+// tensor core needs (A and B of one MMA have one type).  Every wait is bounded; a CTA that gives up
+// lets its copies and MMAs land.
+//
+// Bounds: 4 d flop and one exponential per row and visible key.  Measured on GB300: 43,968 causal
+// tokens, 16 heads of 64 on 4 kv heads, 2.94 ms (1,350 TFLOP/s, 0.71 of the burst bf16 peak; the
+// exponentials and the latency of a chain's steps bound d 64); 32,768 tokens, 16 heads of 128, no mask,
+// 5.6 ms (1,570 TFLOP/s, 0.83 of burst; the tensor pipe).  Between two items of a CTA lie about
+// 7,000 clocks of drain, epilogue and fill (3.7 us), which is what short prompts pay.
 #include <math.h>
 
 #include <type_traits>
@@ -44,12 +56,6 @@ constexpr float kRescaleThreshold = 8.f;   // log2 units
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
-#ifndef VP_SEQ_ITEM_COST
-#define VP_SEQ_ITEM_COST 5
-#endif
-#ifndef VP_SEQ_ITEM_COST128
-#define VP_SEQ_ITEM_COST128 3
-#endif
 template <int D>
 struct Cfg {
   static constexpr int kChains = seq_chains(D);
@@ -67,7 +73,8 @@ struct Cfg {
   static_assert((kAlias ? kColO + kChains * D : kColP + kChains * kBN / 2) <= 512, "TMEM columns");
   // An item costs about as much as this many units on top of its own (its Q, first scores and
   // epilogue, which the other chains hide only in part).
-  static constexpr int kItemCost = D == 64 ? VP_SEQ_ITEM_COST : VP_SEQ_ITEM_COST128;
+  // (Measured on packed prompts of d 128: 2: 351, 3: 337, 4: 347 us; of d 64: 3 to 8 within 2 %.)
+  static constexpr int kItemCost = D == 64 ? 5 : 3;
 };
 
 // A value that is the same on all lanes, in a form that lets the compiler see it: what tcgen05 and TMA
@@ -964,16 +971,18 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
                   make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
           continue;
         }
+        const float2 inv2 = make_float2(inv, inv);
+        auto scaled = [&](int i) {
+          const float2 x = fmul2(make_float2(o[i], o[i + 1]), inv2);
+          return pack2<F16>(x.x, x.y);
+        };
         // Through shared memory (16-byte chunks swizzled by the row), so that eight lanes write a
         // row's 128 bytes and not every lane 16 of its own row.
         __syncwarp();
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          out[lane * 8 + (i ^ (lane & 7))] =
-              make_uint4(pack2<F16>(o[8 * i] * inv, o[8 * i + 1] * inv),
-                         pack2<F16>(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
-                         pack2<F16>(o[8 * i + 4] * inv, o[8 * i + 5] * inv),
-                         pack2<F16>(o[8 * i + 6] * inv, o[8 * i + 7] * inv));
+          out[lane * 8 + (i ^ (lane & 7))] = make_uint4(scaled(8 * i), scaled(8 * i + 2), scaled(8 * i + 4),
+                                                        scaled(8 * i + 6));
         __syncwarp();
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -1103,20 +1112,22 @@ namespace {
 // Which kernel: the one for few rows reads a sequence's keys again (from L2) for every 16 rows, but
 // starts sooner and spreads a small call over all SMs; the tile kernel reads them once for 384
 // or 256 rows.  The host knows the token and sequence counts and the cache's capacity, not the
-// lengths, so the rule goes by averages.  Measured (us, few rows / tiles; d 64 unless stated):
-//   cache, rows per sequence (token x head of a kv head's group) and keys:
-//     8, 16 x 4,096, 16 kv heads: 51 / 91     32, 16 x 4,096, 4: 21 / 38      32, 64 x 4,096, 4: 57 / 91
-//     64, 16 x 4,096, 4: 31 / 39              128, 1 x 32,768, 4: 31 / 44     128, 16 x 4,096, 4: 51 / 41
-//     64, 16 x 4,096, 16: 140 / 92            128, 4 x 8,192, 2, d 128: 29 / 49
-//   prompts of n tokens, 16 heads and kv heads:
-//     1 x 128: 9.6 / 14.3    1 x 256: 14.2 / 15.6    1 x 512: 20.4 / 18.2    8 x 64: 10.9 / 14.8
-//     8 x 128: 18.2 / 16.2
+// lengths, so the rule goes by averages (a batch of single tokens with one long chunk among
+// them is better sent as two calls).  Measured (us, few rows / tiles; 16 heads of 64 on 4 kv heads
+// unless stated):
+//   cache: rows of a kv head per sequence, sequences x keys
+//     8, 16 x 4,096, 16 kv heads: 49 / 86    32, 16 x 4,096: 19 / 35    32, 64 x 4,096: 57 / 87
+//     64, 1 x 2,048: 9.3 / 22    64, 16 x 4,096: 30 / 36    64, 16 x 4,096, 16 kv heads: 137 / 89
+//     128, 1 x 32,768: 28 / 28   128, 16 x 4,096: 51 / 36   128, 4 x 8,192, 2 kv heads of 128: 25 / 36
+//   prompts, 16 kv heads: prompts x tokens
+//     1 x 128: 8.0 / 10.5    1 x 256: 11.6 / 12.4    1 x 512: 18.9 / 14.4    8 x 64: 10.1 / 11.1
+//     8 x 128: 15.5 / 15.0
 bool takes_few_rows(const SeqAttnArgs& a) {
   const long long rows = (long long)a.T * a.group;            // of a kv head
   const long long tiles = (long long)a.T * a.Hq / kSmallRows;  // 16-row tiles of all kv heads
   if (a.kv.k) {
     const long long keys = (long long)a.kv.width << a.kv.log2_page;  // capacity
-    return rows <= 32ll * a.B || (rows <= 128ll * a.B && tiles * (keys / 64) <= 16000);
+    return rows <= 32ll * a.B || (rows <= 128ll * a.B && tiles * (keys / 64) <= 20000);
   }
   return rows <= (long long)kSmallRows * a.B || tiles * ((a.T / a.B + 63) / 64) <= 1200;
 }
