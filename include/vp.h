@@ -438,8 +438,8 @@ vp_status vp_rope_append(const vp_attn_dims* dims, const vp_rope_options* rope, 
  *   q, k, v  [T][heads][d] with their strides;  out [T][Hq][d], out_stride
  *   lse      [T][Hq] float or NULL: log of the row's softmax denominator (natural)
  *   ws       vp_attn_workspace_size bytes, contents arbitrary but for its error word (first 4
- *            bytes, zero at first)
- * Tokens past cu[B] are left alone in out and lse.
+ *            bytes, zero at first); calls that may overlap on the GPU need one each
+ * out and lse overlap no input.  Tokens past cu[B] are left alone in out and lse.
  */
 vp_status vp_prompt_attention(const vp_attn_dims* dims, int32_t T, int32_t B, const void* q,
                               int64_t q_stride, const void* k, int64_t k_stride, const void* v,
@@ -451,7 +451,8 @@ vp_status vp_prompt_attention(const vp_attn_dims* dims, int32_t T, int32_t B, co
  * paged cache, which already holds them (vp_rope_append).
  *   kv_len   [B] int32: tokens in the cache, the new ones included
  *   kv       HOST pointer
- * The other arguments are those of vp_prompt_attention.
+ * The other arguments are those of vp_prompt_attention.  The kernel is chosen by averages over the
+ * sequences: a batch of single tokens with one long chunk among them is better sent as two calls.
  */
 vp_status vp_paged_attention(const vp_attn_dims* dims, int32_t T, int32_t B, const void* q,
                              int64_t q_stride, const int32_t* cu, const int32_t* kv_len,

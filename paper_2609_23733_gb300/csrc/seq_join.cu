@@ -25,6 +25,8 @@ __global__ void __launch_bounds__(kThreads)
   constexpr int kRowsCta = kThreads / (kLanes * kSub);       // rows of a CTA at a time
   constexpr int kRows = kTiles ? seq_chains(D) * 128 : kSmallRows;  // rows of a slot
   __shared__ __align__(16) float s_o[kTiles ? 1 : kThreads][4];
+  __shared__ __align__(16) uint2 s_out[kTiles ? kRowsCta : 1][kLanes + 1];  // rows of outputs, padded
+  __shared__ uint16_t* s_dst[kTiles ? kRowsCta : 1];                        // where they go
   __shared__ __align__(8) float2 s_ml[kTiles ? 1 : kThreads];
   pdl_launch_dependents();
   pdl_wait();
@@ -117,16 +119,25 @@ __global__ void __launch_bounds__(kThreads)
         }
       }
     }
-    if (!valid || sub != 0) continue;
-    const int lim = row_limit(tok, y.y, y.z, a.block), head = x.y * a.group + sub_head;
+    const int lim = valid ? row_limit(tok, y.y, y.z, a.block) : 0, head = x.y * a.group + sub_head;
     const float inv = 1.f / l;
     const uint2 packed = lim > 0 ? make_uint2(pack2<F16>(o[0] * inv, o[1] * inv),
                                               pack2<F16>(o[2] * inv, o[3] * inv))
                                  : make_uint2(0u, 0u);
-    *reinterpret_cast<uint2*>(a.out + (int64_t)(y.x + tok) * a.out_stride + head * D + c) = packed;
-    if (a.lse && c == 0)
+    uint16_t* dst = a.out + (int64_t)(y.x + tok) * a.out_stride + head * D;
+    if (valid && sub == 0 && c == 0 && a.lse)
       a.lse[(size_t)(y.x + tok) * a.Hq + head] =
           lim > 0 ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+    if (kTiles) {  // rows written whole, by neighbouring threads
+      if (base != (int)blockIdx.y * kRowsCta) __syncthreads();
+      s_out[tid % kRowsCta][tid / kRowsCta] = packed;
+      if (c == 0) s_dst[tid % kRowsCta] = valid ? dst : nullptr;
+      __syncthreads();
+      uint16_t* to = s_dst[tid / kLanes];
+      if (to) *reinterpret_cast<uint2*>(to + (tid % kLanes) * 4) = s_out[tid / kLanes][tid % kLanes];
+    } else if (valid && sub == 0) {
+      *reinterpret_cast<uint2*>(dst + c) = packed;
+    }
   }
 }
 

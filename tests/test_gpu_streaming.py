@@ -558,3 +558,39 @@ def test_calls_in_a_graph_follow_their_inputs():
         out.zero_()
         step()
         assert torch.equal(got, out)
+
+
+@pytest.mark.parametrize("n,page", [(1, 16), (40, 64)])
+def test_many_sequences(n, page):
+    """More sequences than a CTA has threads (the scans of the lengths go in rounds), some of them empty."""
+    B, hq, hkv, d = 700, 4, 1, 64
+    rng = np.random.default_rng(n)
+    ql = [int(x) for x in rng.integers(0, n + 1, B)]
+    kl = [int(m + x) if i % 5 else m for i, (m, x) in enumerate(zip(ql, rng.integers(0, 200, B)))]
+    dims = vpb.attn_dims(hq, hkv, d)
+    T = sum(ql)
+    c = Cache(12, kl, hkv, d, page, BF)
+    q = _randn(5, T, hq, d, dtype=BF)
+    ws = _dirty_ws(dims, T, B)
+    out, lse = torch.full_like(q, float("nan")), torch.full((T, hq), float("nan"), device="cuda")
+    vpb.vp_paged_attention(dims, q, _cu(ql), c.kv_len, c.kv, out, lse, ws)
+    assert vpb.vp_read_device_error(ws) == 0
+    qd, od, ld = _f64(q), _f64(out), _f64(lse)
+    t = 0
+    for b, (m, length) in enumerate(zip(ql, kl)):
+        if m:
+            kd, vd = c.dense[b]
+            want = so.seq_attention(qd[t:t + m], _f64(kd), _f64(vd), so.row_limits(m, length, 1), 0.125)
+            _check_attention(od[t:t + m], ld[t:t + m], want, BF, length, 6.0)
+        t += m
+    # prompts: the same query rows over themselves
+    k = _randn(6, T, hkv, d, dtype=BF)
+    vpb.vp_prompt_attention(dims, q, k, k, _cu(ql), out, lse, ws)
+    assert vpb.vp_read_device_error(ws) == 0
+    kd, od, ld = _f64(k), _f64(out), _f64(lse)
+    t = 0
+    for m in ql:
+        if m:
+            r = slice(t, t + m)
+            _check_attention(od[r], ld[r], so.seq_attention(qd[r], kd[r], kd[r], so.row_limits(m, m, 1), 0.125), BF, m, 6.0)
+        t += m
