@@ -73,8 +73,8 @@ struct Cfg {
   static_assert((kAlias ? kColO + kChains * D : kColP + kChains * kBN / 2) <= 512, "TMEM columns");
   // An item costs about as much as this many units on top of its own (its Q, first scores and
   // epilogue, which the other chains hide only in part).
-  // (Measured on packed prompts of d 128: 2: 351, 3: 337, 4: 347 us; of d 64: 3 to 8 within 2 %.)
-  static constexpr int kItemCost = D == 64 ? 5 : 3;
+  // (Measured on packed prompts of d 128: 2: 351, 3: 337, 4: 347 us; of 8 views, d 64: 5: 261, 6: 255, 8: 257 us.)
+  static constexpr int kItemCost = D == 64 ? 6 : 3;
 };
 
 // A value that is the same on all lanes, in a form that lets the compiler see it: what tcgen05 and TMA
