@@ -39,11 +39,31 @@ struct RopeAppendArgs {
 };
 cudaError_t launch_rope_append(const RopeAppendArgs& a, int num_sms, cudaStream_t st);
 
+// Division of 0 <= n < 2^31 by a number the host knows, as a multiplication (round-up method: with s =
+// ceil(log2 d) and mul = ceil(2^(31 + s) / d) < 2^32, floor(n mul / 2^(31 + s)) = floor(n / d) for all
+// such n, since mul d - 2^(31 + s) < d <= 2^s).
+struct FastDiv {
+  uint32_t mul = 0, shift = 0;  // mul 0: d = 1
+  FastDiv() = default;
+  explicit FastDiv(uint32_t d) {
+    if (d <= 1) return;
+    while ((1u << shift) < d && shift < 31) ++shift;  // d <= 2^31
+    mul = (uint32_t)(((1ull << (31 + shift)) + d - 1) / d);
+    --shift;  // the product's upper word is shifted by 31 + s - 32
+  }
+#ifdef __CUDACC__
+  __device__ __forceinline__ int operator()(int n) const {
+    return mul ? (int)(__umulhi((uint32_t)n, mul) >> shift) : n;
+  }
+#endif
+};
+
 struct SeqAttnArgs {
   int T, B, Hq, Hkv, group, d, fp16;
   int block;
   int chain_tokens;          // tokens of a chain (128 / group rows each)
   int block_chains;          // > 0: chains start anew at every mask block, this many per block
+  FastDiv by_group, by_block, by_chain_tokens, by_block_chains;
   float scale_log2;          // scale x log2(e)
   const uint16_t* q;
   int64_t q_stride;
@@ -128,9 +148,10 @@ __device__ __forceinline__ Seq load_seq(const SeqAttnArgs& a, int b) {
 }
 
 // Keys [0, lim) are visible to new token i (0 <= i < ql).  lim <= 0: none.
-__device__ __forceinline__ int row_limit(int i, int ql, int kl, int block) {
-  if (block == 0) return kl;
-  const int rest = ql - i, step = block - i % block;  // both at least 1
+__device__ __forceinline__ int row_limit(const SeqAttnArgs& a, int i, int ql, int kl) {
+  if (a.block == 0) return kl;
+  if (a.block == 1) return kl - ql + i + 1;
+  const int rest = ql - i, step = a.block - (i - a.by_block(i) * a.block);  // both at least 1
   return kl - ql + i + min(rest, step);
 }
 
@@ -138,21 +159,21 @@ __device__ __forceinline__ int row_limit(int i, int ql, int kl, int block) {
 // do not run across mask blocks, so that all rows of a chain see the same keys.
 __device__ __forceinline__ int count_chains(const SeqAttnArgs& a, int ql) {
   const int n = a.chain_tokens;
-  if (a.block_chains == 0) return (ql + n - 1) / n;  // ql <= 2^30
-  const int full = ql / a.block;
-  return full * a.block_chains + (ql - full * a.block + n - 1) / n;
+  if (a.block_chains == 0) return a.by_chain_tokens(ql + n - 1);  // ql <= 2^30
+  const int full = a.by_block(ql);
+  return full * a.block_chains + a.by_chain_tokens(ql - full * a.block + n - 1);
 }
 __device__ __forceinline__ int chain_start(const SeqAttnArgs& a, int chain) {
   if (a.block_chains == 0) return chain * a.chain_tokens;
-  const int full = chain / a.block_chains;
+  const int full = a.by_block_chains(chain);
   return full * a.block + (chain - full * a.block_chains) * a.chain_tokens;
 }
 // One past the chain's last token.
 __device__ __forceinline__ int chain_end(const SeqAttnArgs& a, int chain, int ql) {
-  const int start = chain_start(a, chain);
-  int end = min(start + a.chain_tokens, ql);
-  if (a.block_chains) end = min(end, (chain / a.block_chains + 1) * a.block);
-  return end;
+  if (a.block_chains == 0) return min((chain + 1) * a.chain_tokens, ql);
+  const int full = a.by_block_chains(chain);
+  const int start = full * a.block + (chain - full * a.block_chains) * a.chain_tokens;
+  return min(min(start + a.chain_tokens, (full + 1) * a.block), ql);
 }
 
 // The last sequence b < B with cu[b] <= t (0 if there is none): the owner of token t where cu

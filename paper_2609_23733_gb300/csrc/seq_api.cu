@@ -90,6 +90,10 @@ SeqAttnArgs make_args(const vp_attn_dims* dm, int32_t T, int32_t B, const void* 
     const int64_t n = (dm->block + a.chain_tokens - 1) / a.chain_tokens;
     if (16 * (n * a.chain_tokens - dm->block) <= dm->block && n < (1 << 20)) a.block_chains = (int)n;
   }
+  a.by_group = FastDiv(a.group);
+  a.by_block = FastDiv(a.block);
+  a.by_chain_tokens = FastDiv(a.chain_tokens);
+  a.by_block_chains = FastDiv(a.block_chains);
   a.scale_log2 = dm->scale * 1.4426950408889634f;
   a.q = static_cast<const uint16_t*>(q);
   a.q_stride = q_stride;

@@ -83,8 +83,8 @@ __device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, 
 
 // Key tiles that a token sees.
 template <int kBN>
-__device__ __forceinline__ int tiles_seen(int token, const Seq& s, int block) {
-  const int lim = row_limit(token, s.ql, s.kl, block);
+__device__ __forceinline__ int tiles_seen(const SeqAttnArgs& a, int token, const Seq& s) {
+  const int lim = row_limit(a, token, s.ql, s.kl);
   return lim > 0 ? ceil_div(lim, kBN) : 0;
 }
 
@@ -93,7 +93,7 @@ __device__ __forceinline__ int tiles_seen(int token, const Seq& s, int block) {
 template <class C>
 __device__ __forceinline__ int tile_units(const SeqAttnArgs& a, int c0, const Seq& s) {
   const int last = min(c0 + C::kChains, count_chains(a, s.ql)) - 1;
-  return max(1, tiles_seen<C::kBN>(chain_end(a, last, s.ql) - 1, s, a.block));
+  return max(1, tiles_seen<C::kBN>(a, chain_end(a, last, s.ql) - 1, s));
 }
 
 // ------------------------------------------------------------------ runs of units
@@ -120,8 +120,8 @@ __device__ __forceinline__ Chain chain_of(const SeqAttnArgs& a, const Item& it, 
     x.t0 = chain_start(a, it.c0 + c);
     x.t1 = chain_end(a, it.c0 + c, it.ql);
     const Seq s{it.q0, it.ql, it.kl};
-    x.n = min(max(tiles_seen<kBN>(x.t1 - 1, s, a.block) - it.j0, 0), it.nk);
-    x.hidden_from = max(row_limit(x.t0, s.ql, s.kl, a.block), 0);
+    x.n = min(max(tiles_seen<kBN>(a, x.t1 - 1, s) - it.j0, 0), it.nk);
+    x.hidden_from = max(row_limit(a, x.t0, s.ql, s.kl), 0);
   }
   return x;
 }
@@ -209,66 +209,84 @@ struct TileSmem {
   Chain chain[kItemRing][C::kChains];
 };
 
-// Inclusive scan of v over the CTA's threads; *total: the sum.  s_warp: one value per warp.
-__device__ __forceinline__ long long cta_scan(long long v, long long* s_warp, long long* total) {
-  const int lane = lane_id(), w = warp_id(), n = blockDim.x / 32;
+// Inclusive scan of v over the CTA's 32 kWarps threads; *total: the sum.  s_warp: one value per warp.
+template <int kWarps, class T>
+__device__ __forceinline__ T cta_scan(T v, T* s_warp, T* total) {
+  const int lane = lane_id(), w = warp_id();
 #pragma unroll
   for (int k = 1; k < 32; k <<= 1) {
-    const long long u = __shfl_up_sync(0xffffffffu, v, k);
+    const T u = __shfl_up_sync(0xffffffffu, v, k);
     if (lane >= k) v += u;
   }
   __syncthreads();
   if (lane == 31) s_warp[w] = v;
   __syncthreads();
-  long long t = 0;
-  for (int i = 0; i < n; ++i) {
-    if (i == w) v += t;
-    t += s_warp[i];
+  T t = 0;
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) {
+    const T x = s_warp[i];
+    if (i < w) v += x;
+    t += x;
   }
   *total = t;
   return v;
 }
 
+// x / y of non-negative values; 64-bit division only where it takes it.
+__device__ __forceinline__ long long div64(long long x, long long y) {
+  return (x | y) >> 32 ? x / y : (long long)((uint32_t)x / (uint32_t)y);
+}
+
 // The extents of all tiles in order: on_total(sum of them), then fn(b, c0, seq, extent of an item, extent
 // before the tile) for every tile, each on one thread.  One pass over the tiles where there are
-// no more sequences and tiles than threads, else two.  Called by all threads; s_seq, s_warp: scratch
-// for blockDim sequences and warps.
+// no more sequences and tiles than threads, else two.  Called by all threads; s_seq: scratch of 16 bytes
+// per thread and 4 per warp, s_warp: 8 per warp.
 template <class C, class Total, class Fn>
 __device__ __forceinline__ void scan_tiles(const SeqAttnArgs& a, int4* s_seq, long long* s_warp,
                                            Total on_total, Fn fn) {
-  constexpr int kChains = C::kChains;
-  const int tid = threadIdx.x, n = blockDim.x;
+  constexpr int kChains = C::kChains, n = C::kThreads, kWarps = n / 32;
+  const int tid = threadIdx.x;
+  int* s_int = reinterpret_cast<int*>(s_seq + n);
   bool last = false;  // the pass that calls fn
   for (int pass = 0; pass < 2; ++pass) {
     long long before = 0;
     for (int b0 = 0; b0 < a.B; b0 += n) {
       Seq s{0, 0, 0};
-      if (b0 + tid < a.B) s = load_seq(a, b0 + tid);
-      long long tiles;
-      const long long end = cta_scan(ceil_div(count_chains(a, s.ql), kChains), s_warp, &tiles);
-      s_seq[tid] = make_int4(s.q0, s.ql, s.kl, (int)end);  // .w: tiles up to this sequence's last
-      __syncthreads();
+      int tiles;
+      if (a.B == 1) {  // no search
+        s = load_seq(a, 0);
+        tiles = ceil_div(count_chains(a, s.ql), kChains);
+      } else {
+        if (b0 + tid < a.B) s = load_seq(a, b0 + tid);
+        const int end = cta_scan<kWarps>(ceil_div(count_chains(a, s.ql), kChains), s_int, &tiles);
+        s_seq[tid] = make_int4(s.q0, s.ql, s.kl, end);  // .w: tiles up to this sequence's last
+        __syncthreads();
+      }
       const bool once = a.B <= n && tiles <= n;
       for (int w0 = 0; w0 < tiles; w0 += n) {
         const int w = w0 + tid;
         int lo = 0, c0 = 0;
         long long u = 0;
         if (w < tiles) {
-          int hi = min(n, a.B - b0) - 1;  // the first sequence with .w > w
-          while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (s_seq[mid].w > w)
-              hi = mid;
-            else
-              lo = mid + 1;
+          if (a.B == 1) {
+            c0 = w * kChains;
+          } else {
+            int hi = min(n, a.B - b0) - 1;  // the first sequence with .w > w
+            while (lo < hi) {
+              const int mid = (lo + hi) >> 1;
+              if (s_seq[mid].w > w)
+                hi = mid;
+              else
+                lo = mid + 1;
+            }
+            const int4 x = s_seq[lo];
+            s = Seq{x.x, x.y, x.z};
+            c0 = (w - (x.w - ceil_div(count_chains(a, s.ql), kChains))) * kChains;
           }
-          const int4 x = s_seq[lo];
-          s = Seq{x.x, x.y, x.z};
-          c0 = (w - (x.w - ceil_div(count_chains(a, s.ql), kChains))) * kChains;
           u = tile_units<C>(a, c0, s) + C::kItemCost;
         }
         long long total;
-        const long long upto = cta_scan(u * a.Hkv, s_warp, &total);
+        const long long upto = cta_scan<kWarps>(u * a.Hkv, s_warp, &total);
         if (once) {
           on_total(total);
           last = true;
@@ -381,7 +399,7 @@ __device__ __forceinline__ void find_run(const SeqAttnArgs& a, const SeqScratch&
   const int P = gridDim.x, cta = blockIdx.x;
   long long per = 0, near = 0, x0 = 0, x1 = 0;
   auto on_total = [&](long long total) {
-    per = (total + P - 1) >> 32 ? (total + P - 1) / P : (long long)((uint32_t)(total + P - 1) / (uint32_t)P);
+    per = div64(total + P - 1, P);
     near = max(per / 128, kItemCost + 4ll);
     x0 = cta * per;
     x1 = x0 + per;
@@ -396,7 +414,7 @@ __device__ __forceinline__ void find_run(const SeqAttnArgs& a, const SeqScratch&
   scan_tiles<C>(a, s_seq, s_warp, on_total, [&](int b, int c0, const Seq& s, int n, long long before) {
     const long long end = before + (long long)n * a.Hkv;
     if (before <= x0 && x0 < end) {
-      const int h = (int)((x0 - before) / n);
+      const int h = (int)div64(x0 - before, n);
       const long long first = before + (long long)h * n, x = snap(x0, first, n, near);
       s_begin = x;
       run->b = b;
@@ -405,12 +423,12 @@ __device__ __forceinline__ void find_run(const SeqAttnArgs& a, const SeqScratch&
       run->j0 = x == first ? 0 : (int)(x - first) - kItemCost;  // all: from the next item on
     }
     if (before <= x1 && x1 < end) {
-      const int h = (int)((x1 - before) / n);
+      const int h = (int)div64(x1 - before, n);
       const long long first = before + (long long)h * n, x = snap(x1, first, n, near);
       s_end = x;
       if (x > first && x < first + n && x0 - first < near) {
         // The cuts k per of this item that stay: first + near <= k per <= first + n - near.
-        const int last = (int)((first + n - near) / per);
+        const int last = (int)div64(first + n - near, per);
         s_rec[0] = make_int4(last - cta + 1, h, c0, b);
         s_rec[1] = make_int4(s.q0, s.ql, s.kl, 0);
         s_first = first;
@@ -483,7 +501,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, sm.tmem_base, 0);
 
-  const int group = prm.group, block = prm.block, tpt = prm.chain_tokens;
+  const int group = prm.group, tpt = prm.chain_tokens;
 
   if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kCtrlRegs));
   if (warp == 0) {
@@ -526,19 +544,19 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
           q_last = ic * kChains + c;
         }
       };
-      load_q(0, 1);
-      if (!ok) break;
-      if (walk.left <= 0) {
-        load_q(1, kChains);
-        break;
-      }
       // Page ids: lane l holds that of page first + l; `next` the 32 after them.
-      const int n_pages = kPaged ? (it.kl + ps - 1) >> log2p : 0;
+      const int n_pages = kPaged && walk.left > 0 ? (it.kl + ps - 1) >> log2p : 0;
       const int32_t* table = kPaged ? prm.kv.table + (size_t)it.b * prm.kv.width : nullptr;
       int first = kPaged ? (it.j0 * kBN) >> log2p : 0, window = 0, next = 0;
       if (kPaged) {
         if (first + lane < n_pages) window = table[first + lane];
         if (first + 32 + lane < n_pages) next = table[first + 32 + lane];
+      }
+      load_q(0, 1);
+      if (!ok) break;
+      if (walk.left <= 0) {
+        load_q(1, kChains);
+        break;
       }
       for (int jj = 0; jj < it.nk; ++jj, ++lc) {
         const int j = it.j0 + jj, st = lc % kStages;
@@ -802,7 +820,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
     const uint32_t t_s = tmem + lane_off + C::kColS + c * kBN;
     const uint32_t t_o = tmem + lane_off + C::kColO + c * D;
     const uint32_t t_p = tmem + lane_off + C::kColP + c * C::kPitchP;
-    const int row_tok = row / group, row_head = row - row_tok * group;
+    const int row_tok = prm.by_group(row), row_head = row - row_tok * group;
     const bool flip = prm.scale_log2 < 0.f;  // scores are negated, so that the maximum is the scores'
     const float cs = fmaxf(fabsf(prm.scale_log2), 1e-30f);
     uint32_t g = 0, lc = 0, oc = 0;  // the chain's tiles, ring tiles, the chain's items
@@ -816,7 +834,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       const Chain ch = sm.chain[ic % kItemRing][c];
       const int n = ch.n, tok = ch.t0 + row_tok;  // this thread's token in its sequence
       const bool valid = row_tok < tpt && tok < ch.t1;
-      const int lim = valid ? row_limit(tok, it.ql, it.kl, block) : 0;
+      const int lim = valid ? row_limit(prm, tok, it.ql, it.kl) : 0;
       const int masked_from = ch.hidden_from / kBN;  // the first tile with a hidden key
       const bool active = __any_sync(0xffffffffu, valid);
       float m = kUnset, lsum = 0.f;

@@ -44,14 +44,14 @@ __global__ void __launch_bounds__(kThreads)
     int tok, sub_head;
     bool valid;
     if (kTiles) {  // chain, row of the chain
-      const int chain = x.z + r / 128, row = r % 128, t = row / a.group;
+      const int chain = x.z + r / 128, row = r % 128, t = a.by_group(row);
       valid = chain < count_chains(a, y.y) && t < a.chain_tokens;
       tok = (valid ? chain_start(a, chain) : 0) + t;
       sub_head = row - t * a.group;
       valid = valid && tok < chain_end(a, chain, y.y);
     } else {
       const int row = x.z * kSmallRows + r;
-      tok = row / a.group;
+      tok = a.by_group(row);
       sub_head = row - tok * a.group;
       valid = tok < y.y;
     }
@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(kThreads)
         }
       }
     }
-    const int lim = valid ? row_limit(tok, y.y, y.z, a.block) : 0, head = x.y * a.group + sub_head;
+    const int lim = valid ? row_limit(a, tok, y.y, y.z) : 0, head = x.y * a.group + sub_head;
     const float inv = 1.f / l;
     const uint2 packed = lim > 0 ? make_uint2(pack2<F16>(o[0] * inv, o[1] * inv),
                                               pack2<F16>(o[2] * inv, o[3] * inv))

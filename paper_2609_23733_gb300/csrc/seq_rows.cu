@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
     tma_prefetch_desc(&tmap_k);
     tma_prefetch_desc(&tmap_v);
   }
-  const int Hkv = prm.Hkv, group = prm.group, block = prm.block;
+  const int Hkv = prm.Hkv, group = prm.group;
   pdl_wait();  // what is ahead in the stream: the inputs are there, and the last call's join is over
   Place pl;
   const long long total = find_place(prm, &pl, scratch);  // its barriers also publish the mbarriers
@@ -341,10 +341,10 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int row = rt * kRows + r0 + 8 * i;
-        tok[i] = row / group;
+        tok[i] = prm.by_group(row);
         head[i] = h * group + row - tok[i] * group;
         valid[i] = tok[i] < s.ql;
-        lim[i] = valid[i] ? row_limit(tok[i], s.ql, s.kl, block) : 0;
+        lim[i] = valid[i] ? row_limit(prm, tok[i], s.ql, s.kl) : 0;
         const uint16_t* q = prm.q + (int64_t)(s.q0 + tok[i]) * prm.q_stride + head[i] * D + 2 * tq;
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
@@ -352,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
           qf[kk][2 + i] = valid[i] ? *reinterpret_cast<const uint32_t*>(q + kk * 16 + 8) : 0u;
         }
       }
-      const int masked_from = max(row_limit(rt * kRows / group, s.ql, s.kl, block), 0) / kBN;
+      const int masked_from = max(row_limit(prm, prm.by_group(rt * kRows), s.ql, s.kl), 0) / kBN;
       float m[2] = {kUnset, kUnset}, l[2] = {0.f, 0.f}, o[D / 8][4];
 #pragma unroll
       for (int n = 0; n < D / 8; ++n)
