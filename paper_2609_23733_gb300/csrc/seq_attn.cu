@@ -99,7 +99,7 @@ __device__ __forceinline__ int tile_units(const SeqAttnArgs& a, int c0, const Se
 // ------------------------------------------------------------------ runs of units
 // A CTA's run: the first segment, and its extent in units, kItemCost for every item begun included.
 struct Run {
-  int b, c0, h, j0;
+  int b, c0, h, j0, q0, ql, kl;
   long long units;
 };
 
@@ -139,13 +139,13 @@ struct Walk {
   int here;        // this segment's extent, were its item not cut
   int n_chains;    // of the sequence
 
-  __device__ __forceinline__ void load(const SeqAttnArgs& a) {
-    const Seq s = load_seq(a, it.b);
+  __device__ __forceinline__ void take(const SeqAttnArgs& a, const Seq& s) {
     it.q0 = uniform(s.q0);
     it.ql = uniform(s.ql);
     it.kl = uniform(s.kl);
     n_chains = count_chains(a, it.ql);
   }
+  __device__ __forceinline__ void load(const SeqAttnArgs& a) { take(a, load_seq(a, it.b)); }
   __device__ __forceinline__ void set(const SeqAttnArgs& a) {
     it.all = tile_units<C>(a, it.c0, Seq{it.q0, it.ql, it.kl});
     const int cost = it.j0 == 0 ? kItemCost : 0;
@@ -160,7 +160,7 @@ struct Walk {
     it.part = 0;
     left = __shfl_sync(0xffffffffu, r.units, 0);
     if (left > 0) {
-      load(a);
+      take(a, Seq{r.q0, r.ql, r.kl});
       set(a);
       if (it.nk == 0) {  // from the next item on
         next(a);
@@ -209,27 +209,27 @@ struct TileSmem {
   Chain chain[kItemRing][C::kChains];
 };
 
-// Inclusive scan of v over the CTA's 32 kWarps threads; *total: the sum.  s_warp: one value per warp.
-template <int kWarps, class T>
-__device__ __forceinline__ T cta_scan(T v, T* s_warp, T* total) {
+// Inclusive scan of v over the CTA's 32 kWarps threads; *total: the sum.  v < 2^26, so that a warp's sum
+// fits 32 bits.  s_warp: one value per warp.
+template <int kWarps>
+__device__ __forceinline__ long long cta_scan(int v, int* s_warp, long long* total) {
   const int lane = lane_id(), w = warp_id();
 #pragma unroll
   for (int k = 1; k < 32; k <<= 1) {
-    const T u = __shfl_up_sync(0xffffffffu, v, k);
+    const int u = __shfl_up_sync(0xffffffffu, v, k);
     if (lane >= k) v += u;
   }
   __syncthreads();
   if (lane == 31) s_warp[w] = v;
   __syncthreads();
-  T t = 0;
+  long long t = 0, before = 0;
 #pragma unroll
   for (int i = 0; i < kWarps; ++i) {
-    const T x = s_warp[i];
-    if (i < w) v += x;
-    t += x;
+    if (i == w) before = t;
+    t += s_warp[i];
   }
   *total = t;
-  return v;
+  return before + v;
 }
 
 // x / y of non-negative values; 64-bit division only where it takes it.
@@ -240,13 +240,12 @@ __device__ __forceinline__ long long div64(long long x, long long y) {
 // The extents of all tiles in order: on_total(sum of them), then fn(b, c0, seq, extent of an item, extent
 // before the tile) for every tile, each on one thread.  One pass over the tiles where there are
 // no more sequences and tiles than threads, else two.  Called by all threads; s_seq: scratch of 16 bytes
-// per thread and 4 per warp, s_warp: 8 per warp.
+// per thread and 4 per warp.
 template <class C, class Total, class Fn>
-__device__ __forceinline__ void scan_tiles(const SeqAttnArgs& a, int4* s_seq, long long* s_warp,
-                                           Total on_total, Fn fn) {
+__device__ __forceinline__ void scan_tiles(const SeqAttnArgs& a, int4* s_seq, Total on_total, Fn fn) {
   constexpr int kChains = C::kChains, n = C::kThreads, kWarps = n / 32;
   const int tid = threadIdx.x;
-  int* s_int = reinterpret_cast<int*>(s_seq + n);
+  int* s_warp = reinterpret_cast<int*>(s_seq + n);
   bool last = false;  // the pass that calls fn
   for (int pass = 0; pass < 2; ++pass) {
     long long before = 0;
@@ -258,15 +257,18 @@ __device__ __forceinline__ void scan_tiles(const SeqAttnArgs& a, int4* s_seq, lo
         tiles = ceil_div(count_chains(a, s.ql), kChains);
       } else {
         if (b0 + tid < a.B) s = load_seq(a, b0 + tid);
-        const int end = cta_scan<kWarps>(ceil_div(count_chains(a, s.ql), kChains), s_int, &tiles);
-        s_seq[tid] = make_int4(s.q0, s.ql, s.kl, end);  // .w: tiles up to this sequence's last
+        const int n_tiles = ceil_div(count_chains(a, s.ql), kChains);
+        long long all;  // (2^26 tiles of queries would not fit the GPU's memory)
+        const long long end = cta_scan<kWarps>(min(n_tiles, (1 << 26) - 1), s_warp, &all);
+        tiles = (int)all;
+        s_seq[tid] = make_int4(s.q0, s.ql, s.kl, (int)end);  // .w: tiles up to this sequence's last
         __syncthreads();
       }
       const bool once = a.B <= n && tiles <= n;
       for (int w0 = 0; w0 < tiles; w0 += n) {
         const int w = w0 + tid;
         int lo = 0, c0 = 0;
-        long long u = 0;
+        int u = 0;  // < 2^26: key tiles of at most 2^31 keys
         if (w < tiles) {
           if (a.B == 1) {
             c0 = w * kChains;
@@ -286,12 +288,13 @@ __device__ __forceinline__ void scan_tiles(const SeqAttnArgs& a, int4* s_seq, lo
           u = tile_units<C>(a, c0, s) + C::kItemCost;
         }
         long long total;
-        const long long upto = cta_scan<kWarps>(u * a.Hkv, s_warp, &total);
+        const long long upto = cta_scan<kWarps>(u, s_warp, &total) * a.Hkv;
+        total *= a.Hkv;
         if (once) {
           on_total(total);
           last = true;
         }
-        if (last && u > 0) fn(b0 + lo, c0, s, (int)u, before + upto - u * a.Hkv);
+        if (last && u > 0) fn(b0 + lo, c0, s, u, before + upto - (long long)u * a.Hkv);
         before += total;
       }
       __syncthreads();
@@ -394,7 +397,7 @@ template <class C>
 __device__ __forceinline__ void find_run(const SeqAttnArgs& a, const SeqScratch& sc, int4* s_seq,
                                          Run* run) {
   constexpr int kItemCost = C::kItemCost;
-  __shared__ long long s_warp[32], s_begin, s_end, s_first;
+  __shared__ long long s_begin, s_end, s_first;
   __shared__ int4 s_rec[2];
   const int P = gridDim.x, cta = blockIdx.x;
   long long per = 0, near = 0, x0 = 0, x1 = 0;
@@ -411,7 +414,7 @@ __device__ __forceinline__ void find_run(const SeqAttnArgs& a, const SeqScratch&
     }
     __syncthreads();
   };
-  scan_tiles<C>(a, s_seq, s_warp, on_total, [&](int b, int c0, const Seq& s, int n, long long before) {
+  scan_tiles<C>(a, s_seq, on_total, [&](int b, int c0, const Seq& s, int n, long long before) {
     const long long end = before + (long long)n * a.Hkv;
     if (before <= x0 && x0 < end) {
       const int h = (int)div64(x0 - before, n);
@@ -419,6 +422,9 @@ __device__ __forceinline__ void find_run(const SeqAttnArgs& a, const SeqScratch&
       s_begin = x;
       run->b = b;
       run->c0 = c0;
+      run->q0 = s.q0;
+      run->ql = s.ql;
+      run->kl = s.kl;
       run->h = h;
       run->j0 = x == first ? 0 : (int)(x - first) - kItemCost;  // all: from the next item on
     }
