@@ -181,12 +181,19 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _raw_device = getattr(torch._C, "_cuda_getDevice", None)
 
 
+if _raw_stream is None or _raw_device is None:
+    _raw_stream, _raw_device = (lambda _: torch.cuda.current_stream().cuda_stream), (lambda: 0)
+
+
 def _stream(stream=None):
     if stream is not None:
         return stream.cuda_stream
-    if _raw_stream is not None and _raw_device is not None and torch.cuda.is_initialized():
-        return _raw_stream(_raw_device())
-    return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(_raw_device()) if torch.cuda.is_initialized() else torch.cuda.current_stream().cuda_stream
+
+
+def _stream_of_tensors(stream):
+    """_stream where device tensors are at hand (CUDA is up)."""
+    return _raw_stream(_raw_device()) if stream is None else stream.cuda_stream
 
 
 def dims(N, H=16, d=64, L=64, tau_low=0.01, tau_high=0.20, variant=0) -> VpDims:
@@ -459,6 +466,7 @@ def attn_workspace(dims: VpAttnDims, T: int, B: int, device="cuda") -> torch.Ten
     return ws
 
 
+_byref = ctypes.byref
 _TORCH_DTYPES = {v: k for k, v in VP_DTYPES.items()}
 
 
@@ -492,7 +500,7 @@ def _kv_ref(kv, dims, B):
         raise ValueError("the cache's heads, head dim or type are not those of dims")
     if kv._rows < B:
         raise ValueError(f"the page table has {kv._rows} rows for {B} sequences")
-    return ctypes.byref(kv)
+    return _byref(kv)
 
 
 def vp_rope_append(dims: VpAttnDims, rope: VpRopeOptions, q, k, v, cu, kv_len, positions, kv: VpPagedKv = None,
@@ -505,10 +513,12 @@ def vp_rope_append(dims: VpAttnDims, rope: VpRopeOptions, q, k, v, cu, kv_len, p
     vp, vs = _rows_p(v, kv_shape, dt)
     qo, qos = _rows_p(q_out, q_shape, dt)
     ko, kos = _rows_p(k_out, kv_shape, dt)
-    _check(lib().vp_rope_append(ctypes.byref(dims), ctypes.byref(rope), T, B, qp, qs, kp, ks, vp, vs,
-                                _ints_p(cu, B + 1, "cu"), _ints_p(kv_len, B, "kv_len"),
-                                _ints_p(positions, T, "positions"), _kv_ref(kv, dims, B), qo, qos, ko, kos, _p(ws),
-                                0 if ws is None else ws.numel(), _stream(stream)), "vp_rope_append")
+    wp, wn = (None, 0) if ws is None else _ws_p(ws)
+    st = lib().vp_rope_append(_byref(dims), _byref(rope), T, B, qp, qs, kp, ks, vp, vs, _ints_p(cu, B + 1, "cu"),
+                              _ints_p(kv_len, B, "kv_len"), _ints_p(positions, T, "positions"), _kv_ref(kv, dims, B),
+                              qo, qos, ko, kos, wp, wn, _stream_of_tensors(stream))
+    if st:
+        raise VPError(st, "vp_rope_append")
 
 
 def _ws_p(ws):
@@ -526,25 +536,32 @@ def _lse_p(lse, T, dims):
 
 
 def vp_prompt_attention(dims: VpAttnDims, q, k, v, cu, out, lse, ws, stream=None):
+    """Softmax attention of whole packed prompts over themselves: q, k, v, out [T][heads][d], cu int32 [B + 1],
+    lse float32 [T][Hq] or None, ws from ``attn_workspace``."""
     T, B, d, dt = q.shape[0], cu.numel() - 1, dims.d, _TORCH_DTYPES.get(dims.dtype)
     q_shape, kv_shape = (T, dims.Hq, d), (T, dims.Hkv, d)
     qp, qs = _rows_p(q, q_shape, dt)
     kp, ks = _rows_p(k, kv_shape, dt)
     vp, vs = _rows_p(v, kv_shape, dt)
     op, os_ = _rows_p(out, q_shape, dt)
-    _check(lib().vp_prompt_attention(ctypes.byref(dims), T, B, qp, qs, kp, ks, vp, vs, _ints_p(cu, B + 1, "cu"), op,
-                                     os_, _lse_p(lse, T, dims), *_ws_p(ws), _stream(stream)),
-           "vp_prompt_attention")
+    st = lib().vp_prompt_attention(_byref(dims), T, B, qp, qs, kp, ks, vp, vs, _ints_p(cu, B + 1, "cu"), op,
+                                   os_, _lse_p(lse, T, dims), *_ws_p(ws), _stream_of_tensors(stream))
+    if st:
+        raise VPError(st, "vp_prompt_attention")
 
 
 def vp_paged_attention(dims: VpAttnDims, q, cu, kv_len, kv: VpPagedKv, out, lse, ws, stream=None):
+    """Softmax attention of new tokens (chunks or single tokens, already appended) over the paged cache; kv_len
+    int32 [B] counts them in.  The rest as in ``vp_prompt_attention``."""
     T, B = q.shape[0], cu.numel() - 1
     shape, dt = (T, dims.Hq, dims.d), _TORCH_DTYPES.get(dims.dtype)
     qp, qs = _rows_p(q, shape, dt)
     op, os_ = _rows_p(out, shape, dt)
-    _check(lib().vp_paged_attention(ctypes.byref(dims), T, B, qp, qs, _ints_p(cu, B + 1, "cu"),
-                                    _ints_p(kv_len, B, "kv_len"), _kv_ref(kv, dims, B), op, os_,
-                                    _lse_p(lse, T, dims), *_ws_p(ws), _stream(stream)), "vp_paged_attention")
+    st = lib().vp_paged_attention(_byref(dims), T, B, qp, qs, _ints_p(cu, B + 1, "cu"),
+                                  _ints_p(kv_len, B, "kv_len"), _kv_ref(kv, dims, B), op, os_,
+                                  _lse_p(lse, T, dims), *_ws_p(ws), _stream_of_tensors(stream))
+    if st:
+        raise VPError(st, "vp_paged_attention")
 
 
 def vp_profile_begin(max_launches: int):
