@@ -103,8 +103,8 @@ struct Run {
   long long units;
 };
 
-// A segment of a run: key tiles [j0, j0 + nk) of the tile at chain c0 of sequence b and kv head h, of `all`; the part-th
-// of the run.  nk < 0: no more.
+// A segment of a run: key tiles [j0, j0 + nk), of `all`, of the tile at chain c0 of sequence b and kv
+// head h; the part-th of the run.  nk < 0: no more.
 struct Item {
   int b, c0, h, j0, nk, all, q0, ql, kl, part;
 };
@@ -268,7 +268,7 @@ __device__ __forceinline__ void scan_tiles(const SeqAttnArgs& a, int4* s_seq, To
       for (int w0 = 0; w0 < tiles; w0 += n) {
         const int w = w0 + tid;
         int lo = 0, c0 = 0;
-        int u = 0;  // < 2^26: key tiles of at most 2^31 keys
+        int u = 0;  // < 2^26: key tiles of at most 2^30 keys
         if (w < tiles) {
           if (a.B == 1) {
             c0 = w * kChains;
@@ -844,8 +844,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       const int masked_from = ch.hidden_from / kBN;  // the first tile with a hidden key
       const bool active = __any_sync(0xffffffffu, valid);
       float m = kUnset, lsum = 0.f;
-      // One key tile; kMasked: some row of the item does not see all of it (uniform over the
-      // chains), or the scores are negated.
+      // One key tile; kMasked: some row of the chain may not see all of it, or the scores are negated.
       auto tile = [&](auto masked_const, int jj) -> bool {
         constexpr bool kMasked = decltype(masked_const)::value;
         if (!mbar_wait_warp(&sm.s_full[c], g & 1, err, abort_flag)) return false;
@@ -869,10 +868,16 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
         for (int cc = 1; cc < kBN / 32; ++cc) mx = fmaxf(mx, pmx[cc]);
         const int n_seen = valid ? lim - (it.j0 + jj) * kBN : kBN;
         if (kMasked && __any_sync(0xffffffffu, flip || n_seen < kBN)) {
+          if (flip) {
 #pragma unroll
-          for (int i = 0; i < kBN; ++i) {
-            if (flip) s[i] = -s[i];
-            if (i >= n_seen) s[i] = -INFINITY;
+            for (int i = 0; i < kBN; ++i) s[i] = -s[i];
+          }
+#pragma unroll
+          for (int b = 0; b < kBN; b += 32) {  // a bit per column
+            const int k = min(max(n_seen - b, 0), 32);
+            const uint32_t bits = k == 32 ? 0xffffffffu : (1u << k) - 1u;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) s[b + i] = (bits >> i) & 1u ? s[b + i] : -INFINITY;
           }
           float t[8];
 #pragma unroll
