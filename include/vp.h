@@ -449,7 +449,7 @@ vp_status vp_prompt_attention(const vp_attn_dims* dims, int32_t T, int32_t B, co
 /*
  * vp_paged_attention -- softmax attention of new tokens (a chunk, or single tokens) over the
  * paged cache, which already holds them (vp_rope_append).
- *   kv_len   [B] int32: tokens in the cache, the new ones included
+ *   kv_len   [B] int32: tokens in the cache, the new ones included (at most 2^30)
  *   kv       HOST pointer
  * The other arguments are those of vp_prompt_attention.  The kernel is chosen by averages over the
  * sequences: a batch of single tokens with one long chunk among them is better sent as two calls.

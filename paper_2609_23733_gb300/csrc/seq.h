@@ -7,6 +7,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "common.cuh"
 #include "internal.h"
 
 namespace vp {
@@ -51,11 +52,9 @@ struct FastDiv {
     mul = (uint32_t)(((1ull << (31 + shift)) + d - 1) / d);
     --shift;  // the product's upper word is shifted by 31 + s - 32
   }
-#ifdef __CUDACC__
   __device__ __forceinline__ int operator()(int n) const {
     return mul ? (int)(__umulhi((uint32_t)n, mul) >> shift) : n;
   }
-#endif
 };
 
 struct SeqAttnArgs {
@@ -120,11 +119,6 @@ cudaError_t make_tmap_16bit_4d(CUtensorMap* map, const void* base, bool fp16,
                                const uint64_t dims[4], const uint64_t strides[3],
                                const uint32_t box[4]);
 
-#ifdef __CUDACC__
-}  // namespace vp
-#include "common.cuh"
-namespace vp {
-
 // One sequence: its new tokens [q0, q0 + ql) among the T packed ones, and the keys [0, kl).
 struct Seq {
   int q0, ql, kl;
@@ -137,7 +131,7 @@ __device__ __forceinline__ Seq load_seq(const SeqAttnArgs& a, int b) {
   s.q0 = min(max(c0, 0), a.T);
   s.ql = min(max(c1, s.q0), a.T) - s.q0;
   if (a.kv.k) {
-    const long long cap = (long long)a.kv.width << a.kv.log2_page;
+    const long long cap = min((long long)a.kv.width << a.kv.log2_page, 1ll << 30);
     const int n = a.kv_len[b];
     s.kl = (int)min((long long)max(n, 0), cap);
     if (s.kl != n && a.err) atomicOr(a.err, VP_DEVERR_PAGE);
@@ -250,7 +244,5 @@ __device__ __forceinline__ uint32_t finite2(uint32_t u) {
   if (t & 0x80000000u) u &= 0x0000FFFFu;
   return u;
 }
-
-#endif  // __CUDACC__
 
 }  // namespace vp

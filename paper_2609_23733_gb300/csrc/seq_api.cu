@@ -196,7 +196,8 @@ vp_status vp_prompt_attention(const vp_attn_dims* dims, int32_t T, int32_t B, co
   a.v = static_cast<const uint16_t*>(v);
   a.k_stride = k_stride;
   a.v_stride = v_stride;
-  return from_cuda(launch_seq_attention(a, carve_seq_scratch(ws, dims->d), device_sm_count(), static_cast<cudaStream_t>(stream)));
+  return from_cuda(launch_seq_attention(a, carve_seq_scratch(ws, dims->d), device_sm_count(),
+                                        static_cast<cudaStream_t>(stream)));
 }
 
 vp_status vp_paged_attention(const vp_attn_dims* dims, int32_t T, int32_t B, const void* q,
@@ -216,7 +217,8 @@ vp_status vp_paged_attention(const vp_attn_dims* dims, int32_t T, int32_t B, con
   SeqAttnArgs a = make_args(dims, T, B, q, q_stride, cu, out, out_stride, lse, ws);
   a.kv_len = kv_len;
   a.kv = make_kv(kv);
-  return from_cuda(launch_seq_attention(a, carve_seq_scratch(ws, dims->d), device_sm_count(), static_cast<cudaStream_t>(stream)));
+  return from_cuda(launch_seq_attention(a, carve_seq_scratch(ws, dims->d), device_sm_count(),
+                                        static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

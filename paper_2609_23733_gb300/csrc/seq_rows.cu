@@ -6,10 +6,11 @@
 // mma.sync m16n8k16 with the rows padded to 16 keeps up with HBM and needs no TMEM round
 // trip per tile.  What counts is bytes in flight on every SM and an even cut of the work.
 //
-// The work is the sequence of units (sequence, kv head, 16 rows, 64 keys), an item's (16 rows of a
-// kv head) with kItemCost added; CTA c of P takes the c-th of P equal runs, whatever items they
-// belong to, so that all CTAs end together for any mix of lengths; an item (16 rows of a kv head) that a CTA holds in part leaves a
-// partial result, and seq_join_kernel (a programmatic dependent launch) joins the parts in order.  Each CTA finds its place by a scan over the sequences' lengths.
+// The work is the sequence of units (sequence, kv head, 16 rows, 64 keys), each item (16 rows of a kv
+// head) with kItemCost added; CTA c of P takes the c-th of P equal runs, whatever items they belong
+// to, so that all CTAs end together for any mix of lengths.  An item that a CTA holds in part leaves a
+// partial result, and seq_join_kernel (a programmatic dependent launch) joins the parts in order.
+// Each CTA finds its place by a scan over the sequences' lengths.
 //   warp 4      TMA: K / V tiles through a ring, page by page (page ids read 32 ahead).
 //   warps 0-3   16 keys of every tile each: S = Q K^T (16 x 16), softmax against the warp's own
 //               running maximum (moved when it grows by more than 2^8), O += P V in registers;
