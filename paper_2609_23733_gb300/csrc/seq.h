@@ -141,6 +141,16 @@ __device__ __forceinline__ Seq load_seq(const SeqAttnArgs& a, int b) {
   return s;
 }
 
+// Weights are 2^(score - m); m for a running maximum x (in log2 units: x = mx cs).  bf16: x.  fp16: 2^7
+// below it, since its smallest normal number is 2^-14 and a weight below 2^-24 of the largest would be
+// lost, and those of many keys beside one heavy one add up; with 2^8 for a maximum not yet moved, none
+// passes 2^15.  Rounded up there: 2^(s cs - m) by a fused multiply and add keeps what m's rounding cut
+// off, a factor common to the row's weights, which then only lowers them and cannot make them overflow.
+template <bool F16>
+__device__ __forceinline__ float reference_point(float mx, float cs) {
+  return F16 ? __fmaf_ru(mx, cs, -7.f) : mx * cs;
+}
+
 // Keys [0, lim) are visible to new token i (0 <= i < ql).  lim <= 0: none.
 __device__ __forceinline__ int row_limit(const SeqAttnArgs& a, int i, int ql, int kl) {
   if (a.block == 0) return kl;

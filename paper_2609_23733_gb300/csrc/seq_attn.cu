@@ -40,6 +40,7 @@
 // exponentials and the latency of a chain's steps bound d 64); 32,768 tokens, 16 heads of 128, no mask,
 // 5.6 ms (1,570 TFLOP/s, 0.83 of burst; the tensor pipe).  Between two items of a CTA lie about
 // 7,000 clocks of drain, epilogue and fill (3.7 us), which is what short prompts pay.
+#include <float.h>
 #include <math.h>
 
 #include <type_traits>
@@ -51,7 +52,7 @@ namespace vp {
 namespace {
 
 constexpr int kBM = 128;   // rows of a chain
-constexpr float kUnset = -1e30f;           // running maximum before the first visible key
+constexpr float kUnset = -FLT_MAX;         // reference point before the first visible key
 constexpr float kRescaleThreshold = 8.f;   // log2 units
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
@@ -889,15 +890,15 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
           }
           mx = fmaxf(fmax3(t[0], t[1], t[2]), fmax3(t[3], t[4], fmax3(t[5], t[6], t[7])));
         }
-        const float mx2 = mx * cs;
+        const float to = reference_point<F16>(mx, cs);
         float alpha = 1.f;
         bool need = false;
         if (jj == 0) {
-          m = fmaxf(mx2, kUnset);
-        } else if (mx2 > m + kRescaleThreshold) {
+          m = fmaxf(to, kUnset);
+        } else if (to > m + kRescaleThreshold) {
           need = true;
-          alpha = fast_exp2(m - mx2);
-          m = mx2;
+          alpha = fast_exp2(m - to);
+          m = to;
         }
         const float2 c2 = make_float2(cs, cs), nm = make_float2(-m, -m);
         float2 acc0 = make_float2(0.f, 0.f), acc1 = make_float2(0.f, 0.f);

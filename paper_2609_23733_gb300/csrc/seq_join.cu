@@ -6,6 +6,7 @@
 // ends; a CTA whose entry of the list is empty returns at once.  D / 4 threads per row, 16
 // bytes each; the kernel for few rows may cut an item hundreds of times (one sequence, one kv
 // head), so there kSub groups of threads share a row's parts.
+#include <float.h>
 #include <math.h>
 
 #include "seq.h"
@@ -15,7 +16,7 @@ namespace vp {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr float kUnset = -1e30f;
+constexpr float kUnset = -FLT_MAX;
 
 template <int D, bool F16, bool kTiles>
 __global__ void __launch_bounds__(kThreads)

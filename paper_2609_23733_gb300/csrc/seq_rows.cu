@@ -21,6 +21,7 @@
 // heads of 64 on 4: 40.6 us (5.3 TB/s; the first 2.6 us find the place, the last 4 join the parts).
 // V values that are not finite and not seen by every row are taken out of the tile (0 x inf
 // would reach all rows) and added to the rows that see them.
+#include <float.h>
 #include <math.h>
 
 #include "seq.h"
@@ -33,7 +34,7 @@ constexpr int kRows = kSmallRows;  // rows of an item (an MMA's M)
 constexpr int kBN = 64;            // keys of a unit
 constexpr int kWarps = 4;          // compute warps
 constexpr int kThreads = 32 * (kWarps + 1);
-constexpr float kUnset = -1e30f;
+constexpr float kUnset = -FLT_MAX;
 constexpr float kRescaleThreshold = 8.f;  // log2 units
 // An item costs about as much as this many units on top of its own (its rows' q, the join of the warps):
 // the extent of an item is kItemCost + its units, and cuts within the first kItemCost move to its start.
@@ -393,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
-          mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2));
+          mx[i] = reference_point<F16>(fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2)), 1.f);
         }
         const bool need = mx[0] > m[0] + kRescaleThreshold || mx[1] > m[1] + kRescaleThreshold;
         if (__any_sync(0xffffffffu, need)) {

@@ -449,6 +449,45 @@ def test_growing_scores_and_far_maxima():
             _check_attention(_f64(out), _f64(lse), want, FP, 2000, 6.0)
 
 
+@pytest.mark.parametrize("n,d", [(100, 64), (100, 128), (2048, 64), (2048, 128)])
+@pytest.mark.parametrize("at", [0, 0.5, 1])
+def test_light_keys_beside_a_heavy_one(n, d, at):
+    """One key whose weight is 2^23.4 times that of each other one, with V zero there: what comes out is
+    the light keys' sum.  Tolerance, relative: fp16 keeps a weight, raised by 2^7, to 2^-25, so
+    2^-25 / 2^(7 - 23.4); the output's rounding; scores to 2^-16."""
+    scale = 16.2
+    dims = vpb.attn_dims(2, 1, d, dtype=FP, block=0, scale=scale)
+    q = torch.zeros(n, 2, d, dtype=FP, device="cuda")
+    k, v = torch.zeros(n, 1, d, dtype=FP, device="cuda"), torch.full((n, 1, d), 1000.0, dtype=FP, device="cuda")
+    heavy = int(at * (n - 1))
+    q[..., 0] = 1
+    k[heavy, 0, 0] = 1
+    v[heavy] = 0
+    out, lse, ws = torch.empty_like(q), torch.empty(n, 2, device="cuda"), _dirty_ws(dims, n, 1)
+    vpb.vp_prompt_attention(dims, q, k, v, _cu([n]), out, lse, ws)
+    want, want_lse, _ = so.seq_attention(_f64(q), _f64(k), _f64(v), so.row_limits(n, n, 0), scale)
+    tol = 2.0 ** (scale * math.log2(math.e) - 32) + 2.0 ** -11 + 2.0 ** -16
+    assert np.all(np.abs(_f64(out) - want) <= tol * want)
+    assert np.all(np.abs(_f64(lse) - want_lse) <= 4e-5 + 4e-6 * np.abs(want_lse))
+
+
+@pytest.mark.parametrize("n,d", [(100, 64), (100, 128), (2048, 64), (2048, 128)])
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_past_the_precision_of_32_bits(n, d, dtype, sign):
+    """Scores of 1.1 2^25 and 1.1 2^24: a unit in the last place of the maximum is 4 and more."""
+    dims = vpb.attn_dims(2, 1, d, dtype=dtype, block=1, scale=1.1)
+    q = torch.zeros(n, 2, d, dtype=dtype, device="cuda")
+    k, v = torch.zeros(n, 1, d, dtype=dtype, device="cuda"), _randn(11, n, 1, d, dtype=dtype)
+    q[..., 0] = sign * 4096
+    k[:, 0, 0] = 8192
+    k[::3, 0, 0] = 4096
+    out, lse, ws = torch.empty_like(q), torch.empty(n, 2, device="cuda"), _dirty_ws(dims, n, 1)
+    vpb.vp_prompt_attention(dims, q, k, v, _cu([n]), out, lse, ws)
+    want = so.seq_attention(_f64(q), _f64(k), _f64(v), so.row_limits(n, n, 1), 1.1)
+    _check_attention(_f64(out), _f64(lse), want, dtype, n, float(v.abs().max()))
+
+
 def test_chunks_through_the_cache_equal_the_whole_prompt():
     """A prompt attended at once, and the same tokens appended and attended in chunks and single
     tokens: the rotated q and k are the same bits, the outputs agree within both sides' rounding."""
