@@ -98,6 +98,22 @@ SeqScratch carve_seq_scratch(void* ws, int d);
 constexpr int kSmallRows = 16;
 __host__ __device__ constexpr int small_rows_ctas_per_sm(int d) { return d == 64 ? 3 : 2; }
 constexpr int kMaxRecs = 3 * kMaxCtas;   // CTAs of either kernel, at most
+// Most keys of a sequence, as far as the host knows.
+inline long long most_keys(const SeqAttnArgs& a) {
+  return a.kv.k ? (long long)a.kv.width << a.kv.log2_page : a.T;
+}
+// Items of `rows` rows (token x head of a kv head's group), for sequences of about the mean length.
+inline long long count_items(const SeqAttnArgs& a, int rows) {
+  const long long n = (a.T + a.B - 1) / a.B;
+  return (long long)a.B * a.Hkv * ((n * a.group + rows - 1) / rows);
+}
+// Short items of 16 rows are not cut between CTAs, which saves the join: all of at most 256 keys, and
+// of 512 if there are enough of them for the SMs (us, cut / whole; heads of 64, 4 kv heads,
+// single tokens: 8 x 256: 7.3 / 6.2; 64 x 512: 11.6 / 9.2; 1 x 512: 6.6 / 7.4; 8 x 1,024: 8.2 / 11.8).
+inline bool rows_whole(const SeqAttnArgs& a, int ctas) {
+  const long long keys = most_keys(a);
+  return keys <= 256 || (keys <= 512 && 2 * count_items(a, kSmallRows) >= ctas);
+}
 static_assert(2 * kMaxRecs * kSmallRows <= kMaxSlots * 2 * 128, "its parts fit the scratch");
 cudaError_t launch_seq_rows(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms, cudaStream_t st);
 

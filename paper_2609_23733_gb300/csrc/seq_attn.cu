@@ -1086,8 +1086,7 @@ cudaError_t launch_tiles(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms
   void* args[] = {&mq, &mk, &mv, &aa, &ss};
   e = launch_pdl(tile, dim3(P), C::kThreads, smem, st, args);
   // Items of at most kItemCost + 7 key tiles are never cut (find_run): nothing to join.
-  const long long keys = kPaged ? (long long)a.kv.width << a.kv.log2_page : a.T;
-  if (e != cudaSuccess || keys <= (C::kItemCost + 7) * C::kBN) return e;
+  if (e != cudaSuccess || most_keys(a) <= (C::kItemCost + 7) * C::kBN) return e;
   return launch_seq_join(a, sc, true, P, st);
 }
 
@@ -1142,24 +1141,35 @@ namespace {
 // Which kernel: the one for few rows reads a sequence's keys again (from L2) for every 16 rows, but
 // starts sooner and spreads a small call over all SMs; the tile kernel reads them once for 384
 // or 256 rows.  The host knows the token and sequence counts and the cache's capacity, not the
-// lengths, so the rule goes by averages (a batch of single tokens with one long chunk among
+// lengths, so the rules go by averages (a batch of single tokens with one long chunk among
 // them is better sent as two calls).  Measured (us, few rows / tiles; 16 heads of 64 on 4 kv heads
 // unless stated):
 //   cache: rows of a kv head per sequence, sequences x keys
 //     8, 16 x 4,096, 16 kv heads: 49 / 86    32, 16 x 4,096: 19 / 35    32, 64 x 4,096: 57 / 87
 //     64, 1 x 2,048: 9.3 / 22    64, 16 x 4,096: 30 / 36    64, 16 x 4,096, 16 kv heads: 137 / 89
 //     128, 1 x 32,768: 28 / 28   128, 16 x 4,096: 51 / 36   128, 4 x 8,192, 2 kv heads of 128: 25 / 36
-//   prompts, 16 kv heads: prompts x tokens
-//     1 x 128: 8.0 / 10.5    1 x 256: 11.6 / 12.4    1 x 512: 18.9 / 14.4    8 x 64: 10.1 / 11.1
-//     8 x 128: 15.5 / 15.0
-bool takes_few_rows(const SeqAttnArgs& a) {
-  const long long rows = (long long)a.T * a.group;            // of a kv head
-  const long long tiles = (long long)a.T * a.Hq / kSmallRows;  // 16-row tiles of all kv heads
+//   prompts x tokens, 16 kv heads
+//     1 x 256: 8.4 / 10.8   1 x 400: 11.1 / 12.4   1 x 512: 19.2 / 13.3   8 x 64: 8.4 / 10.3
+//     8 x 128: 15.1 / 13.9  64 x 16: 13.1 / 39.4   64 x 64: 29 / 39 (4 kv heads: 29 / 17)
+bool takes_few_rows(const SeqAttnArgs& a, int num_sms) {
   if (a.kv.k) {
-    const long long keys = (long long)a.kv.width << a.kv.log2_page;  // capacity
-    return rows <= 32ll * a.B || (rows <= 128ll * a.B && tiles * (keys / 64) <= 20000);
+    const long long rows = (long long)a.T * a.group;            // of a kv head
+    const long long tiles = (long long)a.T * a.Hq / kSmallRows;  // 16-row tiles of all kv heads
+    return rows <= 32ll * a.B || (rows <= 128ll * a.B && tiles * (most_keys(a) / 64) <= 20000);
   }
-  return rows <= (long long)kSmallRows * a.B || tiles * ((a.T / a.B + 63) / 64) <= 1200;
+  // Prompts: both kernels' times in us, from the units (16 rows x 64 keys; a tile's rows x its keys) of
+  // all items, or of the items of a CTA where they are not cut.
+  const int ctas = small_rows_ctas_per_sm(a.d) * num_sms, kBN = a.d == 64 ? Cfg<64>::kBN : Cfg<128>::kBN;
+  const int cost = a.d == 64 ? Cfg<64>::kItemCost : Cfg<128>::kItemCost;
+  const long long n = (a.T + a.B - 1) / a.B, items = count_items(a, kSmallRows);
+  const long long tiles = count_items(a, 128 * seq_chains(a.d)), waves = (tiles + num_sms - 1) / num_sms;
+  const double row_units = 4. + (n + 63) / 64, tile_units = cost + (double)((n + kBN - 1) / kBN);
+  const double unit = a.d == 64 ? 0.55 : 0.74, tile_unit = a.d == 64 ? 0.64 : 1.5;
+  const double few = rows_whole(a, ctas) ? 4.5 + unit * row_units * ((items + ctas - 1) / ctas)
+                                         : 7.8 + unit * row_units * items / ctas;
+  const double whole = tile_units < cost + 11. ? tile_units : cost + 11.;  // longer ones are cut
+  const double cut = tile_units * tiles / num_sms;
+  return few <= 6. + tile_unit * (tile_units <= cost + 11. ? whole * waves : cut > whole ? cut : whole);
 }
 
 }  // namespace
@@ -1173,7 +1183,7 @@ cudaError_t launch_seq_attention(const SeqAttnArgs& a, const SeqScratch& sc, int
       {{launch_tiles<128, false, false>, launch_tiles<128, false, true>},
        {launch_tiles<128, true, false>, launch_tiles<128, true, true>}}};
   prof_before(VP_KERNEL_SEQ_ATTN, st);
-  const cudaError_t e = takes_few_rows(a) ? launch_seq_rows(a, sc, num_sms, st)
+  const cudaError_t e = takes_few_rows(a, num_sms) ? launch_seq_rows(a, sc, num_sms, st)
                                           : table[a.d == 128][a.fp16 != 0][a.kv.k != nullptr](a, sc, num_sms, st);
   prof_after(st);
   return e;

@@ -10,7 +10,8 @@
 // head) with kItemCost added; CTA c of P takes the c-th of P equal runs, whatever items they belong
 // to, so that all CTAs end together for any mix of lengths.  An item that a CTA holds in part leaves a
 // partial result, and seq_join_kernel (a programmatic dependent launch) joins the parts in order.
-// Each CTA finds its place by a scan over the sequences' lengths.
+// Each CTA finds its place by a scan over the sequences' lengths.  Short items are kept whole (see
+// rows_whole) and nothing is joined.
 //   warp 4      TMA: K / V tiles through a ring, page by page (page ids read 32 ahead).
 //   warps 0-3   16 keys of every tile each: S = Q K^T (16 x 16), softmax against the warp's own
 //               running maximum (moved when it grows by more than 2^8), O += P V in registers;
@@ -155,12 +156,14 @@ struct Segment {
 };
 
 // The segment at u; false if the run holds none of the item (a cut within its first kItemCost).
-__device__ __forceinline__ bool segment_at(const Place& p, long long u, long long end, Segment* s) {
+// whole: an item belongs to the run that it begins in.
+__device__ __forceinline__ bool segment_at(const Place& p, long long u, long long end, bool whole,
+                                           Segment* s) {
   const long long rel = u - p.base;
   const int ext = p.item();
   const int item = rel >> 32 ? (int)(rel / ext) : (int)((uint32_t)rel / (uint32_t)ext);
   s->item0 = p.base + (long long)item * ext;
-  const int from = (int)(u - s->item0), to = (int)min((long long)ext, end - s->item0);
+  const int from = (int)(u - s->item0), to = whole ? ext : (int)min((long long)ext, end - s->item0);
   if (to < ext && to <= kItemCost) return false;
   s->h = item / p.n_rt;
   s->rt = item - s->h * p.n_rt;
@@ -221,7 +224,7 @@ template <int D, bool F16, bool kPaged>
 __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
     seq_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
                     const __grid_constant__ CUtensorMap tmap_v,
-                    const __grid_constant__ SeqAttnArgs prm, const SeqScratch sc) {
+                    const __grid_constant__ SeqAttnArgs prm, const SeqScratch sc, const bool whole) {
   using C = RowsCfg<D>;
   constexpr int kStages = C::kStages, kHalves = C::kHalves;
   extern __shared__ unsigned char smem_raw[];
@@ -249,9 +252,16 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
   Place pl;
   const long long total = find_place(prm, &pl, scratch);  // its barriers also publish the mbarriers
   const long long per = units_per_cta(total, P);
-  const long long begin = min(cta * per, total), end = min(begin + per, total);
+  long long begin = min(cta * per, total);
+  const long long end = min(begin + per, total);
   if (tid == 0) sc.recs[2 * cta] = make_int4(0, 0, 0, 0);  // until the producer knows better
   if (begin >= end) return;  // uniform
+  if (whole) {  // from the next item's start on
+    const int ext = pl.item(), in = (int)((begin - pl.base) % ext);
+    if (in > 0) begin += ext - in;
+    if (begin >= end) return;  // uniform
+    if (begin - pl.base >= pl.extent(Hkv)) advance(prm, &pl);
+  }
   bool ok = true;
 
   if (warp == kWarps) {
@@ -262,7 +272,7 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
     uint32_t lc = 0;
     for (long long u = begin; u < end && ok;) {
       Segment sg;
-      if (!segment_at(pl, u, end, &sg)) break;
+      if (!segment_at(pl, u, end, whole, &sg)) break;
       const int h = sg.h;
       const int n_pages = kPaged ? (pl.s.kl + ps - 1) >> log2p : 0;
       const int32_t* table = kPaged ? prm.kv.table + (size_t)pl.b * prm.kv.width : nullptr;
@@ -334,7 +344,7 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
     uint32_t lc = 0;
     for (long long u = begin; u < end && ok;) {
       Segment sg;
-      if (!segment_at(pl, u, end, &sg)) break;
+      if (!segment_at(pl, u, end, whole, &sg)) break;
       const int h = sg.h, rt = sg.rt;
       const Seq s = pl.s;
       int tok[2], head[2], lim[2];
@@ -577,11 +587,10 @@ cudaError_t launch_rows(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms,
   if (e != cudaSuccess) return e;
   SeqAttnArgs aa = a;
   SeqScratch ss = sc;
-  void* args[] = {&mk, &mv, &aa, &ss};
+  bool whole = rows_whole(a, P);
+  void* args[] = {&mk, &mv, &aa, &ss, &whole};
   e = launch_pdl(fn, dim3(P), kThreads, smem, st, args);
-  if (e != cudaSuccess) return e;
-  const long long keys = kPaged ? (long long)a.kv.width << a.kv.log2_page : a.T;
-  if (keys <= kBN) return e;  // items of one unit: nothing is cut
+  if (e != cudaSuccess || whole) return e;
   return launch_seq_join(a, sc, false, P, st);
 }
 

@@ -633,3 +633,30 @@ def test_many_sequences(n, page):
             r = slice(t, t + m)
             _check_attention(od[r], ld[r], so.seq_attention(qd[r], kd[r], kd[r], so.row_limits(m, m, 1), 0.125), BF, m, 6.0)
         t += m
+
+
+@pytest.mark.parametrize("d,dtype", [(64, BF), (128, FP)])
+@pytest.mark.parametrize("B,most,hkv", [(50, 511, 12), (3, 256, 2), (90, 130, 3)])
+def test_short_contexts(B, most, hkv, d, dtype):
+    """Caches of few pages, more and fewer items than CTAs, chunks of 0 to 3 tokens."""
+    rng = np.random.default_rng(most)
+    ql = [int(x) for x in rng.integers(0, 4, B)]
+    kl = [max(m, int(x)) for m, x in zip(ql, rng.integers(0, most + 1, B))]
+    kl[B // 2] = most
+    hq = 2 * hkv
+    dims = vpb.attn_dims(hq, hkv, d, dtype=dtype)
+    T = sum(ql)
+    c = Cache(17, kl, hkv, d, 32, dtype)
+    q = _randn(18, T, hq, d, dtype=dtype)
+    ws = _dirty_ws(dims, T, B)
+    out, lse = torch.full_like(q, float("nan")), torch.full((T, hq), float("nan"), device="cuda")
+    vpb.vp_paged_attention(dims, q, _cu(ql), c.kv_len, c.kv, out, lse, ws)
+    assert vpb.vp_read_device_error(ws) == 0
+    qd, od, ld = _f64(q), _f64(out), _f64(lse)
+    t = 0
+    for b, (m, length) in enumerate(zip(ql, kl)):
+        if m:
+            kd, vd = c.dense[b]
+            want = so.seq_attention(qd[t:t + m], _f64(kd), _f64(vd), so.row_limits(m, length, 1), 1 / math.sqrt(d))
+            _check_attention(od[t:t + m], ld[t:t + m], want, dtype, length, float(vd.abs().max()) if length else 0.0)
+        t += m
