@@ -420,8 +420,8 @@ vp_status vp_attn_workspace_size(const vp_attn_dims* dims, int32_t T, int32_t B,
  *   kv_len     [B] int32: lengths after the append (NULL without kv)
  *   positions  [T] int32 (>= 0), or NULL: the slot (without kv: the index in the chunk)
  *   kv         HOST pointer, or NULL: nothing is appended (v may then be NULL)
- *   q_out      rotated q (may be q itself); NULL only if q is
- *   k_out      rotated k, packed (may be k itself), or NULL; needed without kv
+ *   q_out      rotated q (may be q itself, with its stride); NULL only if q is
+ *   k_out      rotated k, packed (may be k itself, with its stride), or NULL; needed without kv
  *   ws         workspace whose error word takes VP_DEVERR_PAGE, or NULL
  * A token whose slot is negative, past the table, or on a page id outside the pool is not
  * written to the cache.  Two tokens of one call never share a slot unless sequences share pages.

@@ -144,6 +144,9 @@ vp_status vp_rope_append(const vp_attn_dims* dims, const vp_rope_options* rope, 
     return VP_ERR_INVALID_ARG;
   }
   if (k_out) VP_TRY(check_rows(k_out, k_out_stride, dims->Hkv, dims->d));
+  // In place: every token where it was.
+  if ((q && q == q_out && q_stride != q_out_stride) || (k == k_out && k_stride != k_out_stride))
+    return VP_ERR_INVALID_ARG;
   if (ws && ws_bytes < 256) return VP_ERR_WORKSPACE;
   if (T == 0) return VP_OK;
   if (!device_is_sm103()) return VP_ERR_UNSUPPORTED_DEVICE;

@@ -160,6 +160,14 @@ def test_append_tensors_and_rotation(lib):
     assert _append(lib, dm, qos=1020) == SHAPE and _append(lib, dm, qos=1028) == ALIGN
 
 
+def test_append_in_place_keeps_the_strides(lib):
+    dm = _dims()
+    assert _append(lib, dm, qs=1024, qos=2048) == INVALID
+    assert _passes(_append(lib, dm, qs=1024, qos=2048, qo=A + (1 << 20)))
+    assert _append(lib, dm, ko=A, ks=256, kos=512) == INVALID
+    assert _passes(_append(lib, dm, ko=A, ks=512, kos=512))
+
+
 def test_struct_layouts():
     assert ctypes.sizeof(vpb.VpAttnDims) == 24
     assert ctypes.sizeof(vpb.VpPagedKv) == 3 * 8 + 3 * 4 + 4
