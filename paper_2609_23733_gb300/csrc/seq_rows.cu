@@ -41,6 +41,11 @@ constexpr float kRescaleThreshold = 8.f;  // log2 units
 // the extent of an item is kItemCost + its units, and cuts within the first kItemCost move to its start.
 // (64 single tokens over 97 to 16,381 keys: 47.4 us without, 43.0 with 1, 40.6 with 2 to 5.)
 constexpr int kItemCost = 4;
+// The same where items are kept whole and there are no more of them than CTAs: runs of one item, so that
+// none has two while another has none (prompts of 1, 16, 261, 4 and 65 tokens, 16 heads of 64: 10.8 ->
+// 9.1 us; with more items than CTAs runs of equal work are better: prompts of 3, 5, 400 and 90
+// tokens, 4 kv heads, 12.2 against 17.2 us).
+constexpr int kWholeCost = 32;
 
 template <int D>
 struct RowsCfg {
@@ -66,7 +71,8 @@ struct Place {
   long long base;    // the extent of all items before it
   Seq s;
   int n_kv, n_rt;    // key tiles, 16-row tiles per kv head
-  __device__ __forceinline__ int item() const { return n_kv + kItemCost; }
+  int cost;          // kItemCost or kWholeCost
+  __device__ __forceinline__ int item() const { return n_kv + cost; }
   __device__ __forceinline__ long long extent(int Hkv) const { return (long long)Hkv * n_rt * item(); }
 };
 
@@ -86,7 +92,8 @@ __device__ __forceinline__ long long units_per_cta(long long total, int P) {
 // The units of all sequences, and the place of this CTA's first one (if it has any): a scan of the
 // lengths by all threads, once where there are no more sequences than threads, else once for
 // the total and once for the place.  scratch: a value per warp.
-__device__ __forceinline__ long long find_place(const SeqAttnArgs& a, Place* place, long long* scratch) {
+__device__ __forceinline__ long long find_place(const SeqAttnArgs& a, int cost, Place* place,
+                                                long long* scratch) {
   __shared__ Place s_place;
   const int tid = threadIdx.x, n = blockDim.x, n_warps = n / 32, lane = lane_id(), w = warp_id();
   if (tid == 0) {
@@ -94,6 +101,7 @@ __device__ __forceinline__ long long find_place(const SeqAttnArgs& a, Place* pla
     s_place.base = 0;
     s_place.s = Seq{0, 0, 0};
     s_place.n_kv = s_place.n_rt = 1;
+    s_place.cost = cost;
   }
   long long all = 0;
   for (int pass = a.B <= n ? 1 : 0; pass < 2; ++pass) {
@@ -102,6 +110,7 @@ __device__ __forceinline__ long long find_place(const SeqAttnArgs& a, Place* pla
       Place p;
       long long mine = 0;
       if (b0 + tid < a.B) {
+        p.cost = cost;
         fill_place(a, b0 + tid, &p);
         mine = p.extent(a.Hkv);
       }
@@ -155,7 +164,7 @@ struct Segment {
   long long item0;  // where the item begins
 };
 
-// The segment at u; false if the run holds none of the item (a cut within its first kItemCost).
+// The segment at u; false if the run holds none of the item (a cut within its first p.cost).
 // whole: an item belongs to the run that it begins in.
 __device__ __forceinline__ bool segment_at(const Place& p, long long u, long long end, bool whole,
                                            Segment* s) {
@@ -164,11 +173,11 @@ __device__ __forceinline__ bool segment_at(const Place& p, long long u, long lon
   const int item = rel >> 32 ? (int)(rel / ext) : (int)((uint32_t)rel / (uint32_t)ext);
   s->item0 = p.base + (long long)item * ext;
   const int from = (int)(u - s->item0), to = whole ? ext : (int)min((long long)ext, end - s->item0);
-  if (to < ext && to <= kItemCost) return false;
+  if (to < ext && to <= p.cost) return false;
   s->h = item / p.n_rt;
   s->rt = item - s->h * p.n_rt;
-  s->t0 = max(from - kItemCost, 0);
-  s->t1 = to - kItemCost;
+  s->t0 = max(from - p.cost, 0);
+  s->t1 = to - p.cost;
   s->part = s->t0 > 0 || s->t1 < p.n_kv;
   return true;
 }
@@ -224,7 +233,8 @@ template <int D, bool F16, bool kPaged>
 __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
     seq_rows_kernel(const __grid_constant__ CUtensorMap tmap_k,
                     const __grid_constant__ CUtensorMap tmap_v,
-                    const __grid_constant__ SeqAttnArgs prm, const SeqScratch sc, const bool whole) {
+                    const __grid_constant__ SeqAttnArgs prm, const SeqScratch sc, const int cost,
+                    const bool whole) {
   using C = RowsCfg<D>;
   constexpr int kStages = C::kStages, kHalves = C::kHalves;
   extern __shared__ unsigned char smem_raw[];
@@ -250,7 +260,7 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
   const int Hkv = prm.Hkv, group = prm.group;
   pdl_wait();  // what is ahead in the stream: the inputs are there, and the last call's join is over
   Place pl;
-  const long long total = find_place(prm, &pl, scratch);  // its barriers also publish the mbarriers
+  const long long total = find_place(prm, cost, &pl, scratch);  // its barriers also publish the mbarriers
   const long long per = units_per_cta(total, P);
   long long begin = min(cta * per, total);
   const long long end = min(begin + per, total);
@@ -588,7 +598,8 @@ cudaError_t launch_rows(const SeqAttnArgs& a, const SeqScratch& sc, int num_sms,
   SeqAttnArgs aa = a;
   SeqScratch ss = sc;
   bool whole = rows_whole(a, P);
-  void* args[] = {&mk, &mv, &aa, &ss, &whole};
+  int cost = whole && count_items(a, kRows) <= P ? kWholeCost : kItemCost;
+  void* args[] = {&mk, &mv, &aa, &ss, &cost, &whole};
   e = launch_pdl(fn, dim3(P), kThreads, smem, st, args);
   if (e != cudaSuccess || whole) return e;
   return launch_seq_join(a, sc, false, P, st);
