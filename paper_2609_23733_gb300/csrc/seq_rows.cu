@@ -264,7 +264,9 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
   const long long per = units_per_cta(total, P);
   long long begin = min(cta * per, total);
   const long long end = min(begin + per, total);
-  if (tid == 0) sc.recs[2 * cta] = make_int4(0, 0, 0, 0);  // until the producer knows better
+  // Nothing cut, until the producer knows better: cleared by the thread that writes the entry below, since
+  // no barrier lies between the two.
+  if (tid == 32 * kWarps) sc.recs[2 * cta] = make_int4(0, 0, 0, 0);
   if (begin >= end) return;  // uniform
   if (whole) {  // from the next item's start on
     const int ext = pl.item(), in = (int)((begin - pl.base) % ext);
