@@ -895,7 +895,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
         bool need = false;
         if (jj == 0) {
           m = fmaxf(to, kUnset);
-        } else if (to > m + kRescaleThreshold) {
+        } else if (to - m > kRescaleThreshold) {  // (m + 8 could round up to `to`)
           need = true;
           alpha = fast_exp2(m - to);
           m = to;

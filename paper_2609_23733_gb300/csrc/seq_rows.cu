@@ -418,7 +418,8 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<D>::kPerSm)
           mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
           mx[i] = reference_point<F16>(fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2)), 1.f);
         }
-        const bool need = mx[0] > m[0] + kRescaleThreshold || mx[1] > m[1] + kRescaleThreshold;
+        // (A difference: m + 8 could round up to mx.)
+        const bool need = mx[0] - m[0] > kRescaleThreshold || mx[1] - m[1] > kRescaleThreshold;
         if (__any_sync(0xffffffffu, need)) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {

@@ -1,5 +1,5 @@
 """Streaming attention on the GPU where its kernels' schedules and number ranges end: items cut between
-CTAs, against the 64-bit definitions (oracle.streaming)."""
+CTAs, large scores, against the 64-bit definitions (oracle.streaming)."""
 import math
 
 import numpy as np
@@ -49,3 +49,36 @@ def test_cut_items_are_joined_on_every_call(kl, hq, hkv, d, dtype):
         same &= (out == first).all() & (lse == first_lse).all()
     assert same.item()
     assert vpb.vp_read_device_error(ws) == 0
+
+
+# ------------------------------------------------------------------------------ large scores
+def _large_scores(k_rows, q_row, n, d, dtype, scale, sign=1, block=1):
+    """A prompt of n tokens whose q and k have a few channels set and the rest zero, checked."""
+    dims = vpb.attn_dims(2, 1, d, dtype=dtype, block=block, scale=scale)
+    q = torch.zeros(n, 2, d, dtype=dtype, device="cuda")
+    k, v = torch.zeros(n, 1, d, dtype=dtype, device="cuda"), _randn(11, n, 1, d, dtype=dtype)
+    for ch, x in enumerate(q_row):
+        q[..., ch] = sign * x
+    for ch, x in enumerate(k_rows):
+        k[:, 0, ch] = x.to(dtype).cuda()
+    out, lse, ws = torch.full_like(q, float("nan")), torch.empty(n, 2, device="cuda"), _dirty_ws(dims, n, 1)
+    vpb.vp_prompt_attention(dims, q, k, v, _cu([n]), out, lse, ws)
+    want = so.seq_attention(_f64(q), _f64(k), _f64(v), so.row_limits(n, n, block), float(np.float32(scale)))
+    _check_attention(_f64(out), _f64(lse), want, dtype, n, float(v.abs().max()))
+
+
+@pytest.mark.parametrize("n,d", [(100, 64), (100, 128), (2048, 64), (2048, 128)])
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("low", [2 ** 27 + 16, 2 ** 27 + 48, 2 ** 28 - 16])
+def test_maximum_that_grows_by_one_unit_in_the_last_place(low, dtype, n, d):
+    """log2 scores of `low` in the first half of the keys and low + 16, the next 32-bit value, in the second:
+    a threshold of 8 added to the first rounds to the second.  Scale times log2(e) is 1 in 32 bits.
+
+    All products are exact (powers of two times 8 bits) and so are their sums (multiples of 16 below
+    2^28); the second half's weights are 2^16 times the first's."""
+    scale = 0.6931472
+    assert np.float32(scale) * np.float32(1.4426950408889634) == 1
+    step = torch.where(torch.arange(n) < n // 2, 0.0, 1.0)
+    base = 2 ** 27 if low < 2 ** 28 - 16 else 2 ** 28
+    _large_scores([torch.full((n,), base / 16384.0), (low - base) / 16.0 + step], [16384.0, 16.0], n, d, dtype, scale,
+                  block=0)
