@@ -64,6 +64,7 @@ struct SeqAttnArgs {
   int block_chains;          // > 0: chains start anew at every mask block, this many per block
   FastDiv by_group, by_block, by_chain_tokens, by_block_chains;
   float scale_log2;          // scale x log2(e)
+  float far_from, far_scale, far_unit;  // the tile kernel's scores past kFarScore (see there)
   const uint16_t* q;
   int64_t q_stride;
   const uint16_t* k;         // prompts: packed keys and values; paged: NULL (in kv)
@@ -135,6 +136,20 @@ cudaError_t make_tmap_16bit_4d(CUtensorMap* map, const void* base, bool fp16,
                                const uint64_t dims[4], const uint64_t strides[3],
                                const uint32_t box[4]);
 
+// The tile kernel takes 2^(s cs - m) in one fused multiply and add, whose product is exact while m has 24
+// bits.  What m's rounding leaves is common to all of a row's weights, and far out it would make all of
+// them 0 or infinite (a unit in m's last place is 64 at 2^29).  Where a tile's largest score is past
+// kFarScore, s far_scale is taken instead, far_scale the power of two from cs up: a product with 24 bits, so
+// m = mx far_scale is exact.  Two different scores lie at least 16 apart there, so a weight w < 1 is below
+// 2^-16 and comes out between w^2 and w.  The log-sum is put back into units of cs.
+constexpr float kFarScore = 1 << 28;
+constexpr float kLeastScale = 1e-30f;  // of the tile kernel's |cs|, so that a hidden score, -inf, stays -inf
+// m in units of cs: a near tile's m is below kFarScore (far_from is a little below kFarScore / cs), a far
+// one's that is below it too has far_unit = 1 to 2^-19.
+__device__ __forceinline__ float near_units(const SeqAttnArgs& a, float m) {
+  return fabsf(m) < kFarScore ? m : m * a.far_unit;
+}
+
 // One sequence: its new tokens [q0, q0 + ql) among the T packed ones, and the keys [0, kl).
 struct Seq {
   int q0, ql, kl;
@@ -161,7 +176,8 @@ __device__ __forceinline__ Seq load_seq(const SeqAttnArgs& a, int b) {
 // below it, since its smallest normal number is 2^-14 and a weight below 2^-24 of the largest would be
 // lost, and those of many keys beside one heavy one add up; with 2^8 for a maximum not yet moved, none
 // passes 2^15.  Rounded up there: 2^(s cs - m) by a fused multiply and add keeps what m's rounding cut
-// off, a factor common to the row's weights, which then only lowers them and cannot make them overflow.
+// off, a factor common to the row's weights, which then only lowers them (2^-16 at most, see kFarScore) and
+// cannot make them overflow.
 template <bool F16>
 __device__ __forceinline__ float reference_point(float mx, float cs) {
   return F16 ? __fmaf_ru(mx, cs, -7.f) : mx * cs;

@@ -95,6 +95,12 @@ SeqAttnArgs make_args(const vp_attn_dims* dm, int32_t T, int32_t B, const void* 
   a.by_chain_tokens = FastDiv(a.chain_tokens);
   a.by_block_chains = FastDiv(a.block_chains);
   a.scale_log2 = dm->scale * 1.4426950408889634f;
+  const float cs = fmaxf(fabsf(a.scale_log2), kLeastScale);
+  int e;
+  const bool power = frexpf(cs, &e) == 0.5f;  // cs in [2^(e - 1), 2^e)
+  a.far_scale = power ? cs : ldexpf(1.f, e < 127 ? e : 127);
+  a.far_unit = cs / a.far_scale;
+  a.far_from = (float)(kFarScore * (1. - 0x1p-20) / cs);
   a.q = static_cast<const uint16_t*>(q);
   a.q_stride = q_stride;
   a.cu = cu;

@@ -829,7 +829,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
     const uint32_t t_p = tmem + lane_off + C::kColP + c * C::kPitchP;
     const int row_tok = prm.by_group(row), row_head = row - row_tok * group;
     const bool flip = prm.scale_log2 < 0.f;  // scores are negated, so that the maximum is the scores'
-    const float cs = fmaxf(fabsf(prm.scale_log2), 1e-30f);
+    const float cs = fmaxf(fabsf(prm.scale_log2), kLeastScale);
     uint32_t g = 0, lc = 0, oc = 0;  // the chain's tiles, ring tiles, the chain's items
     bool ok = true;
     for (uint32_t ic = 0;; ++ic) {
@@ -890,7 +890,8 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
           }
           mx = fmaxf(fmax3(t[0], t[1], t[2]), fmax3(t[3], t[4], fmax3(t[5], t[6], t[7])));
         }
-        const float to = reference_point<F16>(mx, cs);
+        const float mul = fabsf(mx) < prm.far_from ? cs : prm.far_scale;
+        const float to = reference_point<F16>(mx, mul);
         float alpha = 1.f;
         bool need = false;
         if (jj == 0) {
@@ -900,7 +901,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
           alpha = fast_exp2(m - to);
           m = to;
         }
-        const float2 c2 = make_float2(cs, cs), nm = make_float2(-m, -m);
+        const float2 c2 = make_float2(mul, mul), nm = make_float2(-m, -m);
         float2 acc0 = make_float2(0.f, 0.f), acc1 = make_float2(0.f, 0.f);
         uint32_t pk[kBN / 2];
 #pragma unroll
@@ -1037,7 +1038,7 @@ __global__ void __launch_bounds__(Cfg<D>::kThreads, 1)
       if (valid && part) sc.part_ml[slot_chain * kBM + row] = make_float2(m, lsum);
       if (valid && !part && prm.lse)
         prm.lse[(size_t)(it.q0 + tok) * prm.Hq + it.h * group + row_head] =
-            lim > 0 ? (m + log2f(lsum)) * 0.69314718055994531f : -INFINITY;
+            lim > 0 ? (near_units(prm, m) + log2f(lsum)) * 0.69314718055994531f : -INFINITY;
       __syncwarp();
     }
   }

@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(kThreads)
     uint16_t* dst = a.out + (int64_t)(y.x + tok) * a.out_stride + head * D;
     if (valid && sub == 0 && c == 0 && a.lse)
       a.lse[(size_t)(y.x + tok) * a.Hq + head] =
-          lim > 0 ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+          lim > 0 ? ((kTiles ? near_units(a, m) : m) + log2f(l)) * 0.69314718055994531f : -INFINITY;
     if (kTiles) {  // rows written whole, by neighbouring threads
       if (base != (int)blockIdx.y * kRowsCta) __syncthreads();
       s_out[tid % kRowsCta][tid / kRowsCta] = packed;

@@ -82,3 +82,31 @@ def test_maximum_that_grows_by_one_unit_in_the_last_place(low, dtype, n, d):
     base = 2 ** 27 if low < 2 ** 28 - 16 else 2 ** 28
     _large_scores([torch.full((n,), base / 16384.0), (low - base) / 16.0 + step], [16384.0, 16.0], n, d, dtype, scale,
                   block=0)
+
+
+@pytest.mark.parametrize("n,d", [(100, 64), (100, 128), (2048, 64), (2048, 128)])
+@pytest.mark.parametrize("dtype,top", [(FP, (59.5, 59.5)), (FP, (30016.0, 20000.0)), (FP, (60000.0, 40000.0)),
+                                       (BF, (30080.0, 20096.0)), (BF, (2.2e6, 3.3e6)), (BF, (3.0e9, 2.1e9)),
+                                       (BF, (1.1e15, 0.9e15))])
+@pytest.mark.parametrize("scale", [1.1, 0.77, 2.9])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_of_any_size(n, d, dtype, top, scale, sign):
+    """Scores up to 10^30, far past where a unit in the last place of one is a whole power of two of its
+    weight: equal scores have equal weights and the largest one's is not lost."""
+    x = torch.full((n,), top[1])
+    x[::3] = top[1] / 2
+    _large_scores([x], [top[0]], n, d, dtype, scale, sign)
+
+
+@pytest.mark.parametrize("n,d", [(100, 64), (2048, 64), (2048, 128)])
+@pytest.mark.parametrize("dtype,top", [(FP, (30016.0, 60000.0)), (BF, (3.0e9, 2.1e9))])
+@pytest.mark.parametrize("scale", [0.6931472, 0.77, 2.9])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("order", ["rising", "mixed"])
+def test_scores_from_small_to_far(n, d, dtype, top, scale, sign, order):
+    """Keys whose scores run from 0 to 10^9 and more, small, far and between in one row, in steps that grow
+    faster than a unit in the last place of the scores."""
+    x = torch.linspace(0, 1, n).to(dtype).float().pow(3) * top[1]
+    if order == "mixed":
+        x = x[torch.randperm(n, generator=torch.Generator().manual_seed(n))]
+    _large_scores([x], [top[0]], n, d, dtype, scale, sign)
