@@ -73,6 +73,8 @@ class ViewStream:
         if max(after) > self.max_tokens:
             raise ValueError(f"the cache holds {self.max_tokens} tokens of a sequence")
         T, first = x.shape[0], max(self.held) == 0
+        if T == 0:  # nobody has new tokens
+            return x
         cu = torch.tensor([sum(lens[:b]) for b in range(n_seqs + 1)], dtype=torch.int32).cuda()
         kv_len = torch.tensor(after, dtype=torch.int32).cuda()
         need = vp.vp_attn_workspace_size(self.dims, T, n_seqs)

@@ -131,12 +131,14 @@ vp_status vp_rope_append(const vp_attn_dims* dims, const vp_rope_options* rope, 
                          size_t ws_bytes, void* stream) {
   VP_TRY(check_attn_dims(dims));
   VP_TRY(check_counts(T, B));
-  if (!rope || !cu || !q != !q_out) return VP_ERR_INVALID_ARG;
+  if (!rope) return VP_ERR_INVALID_ARG;
   if (rope->rot_dim < 0 || rope->rot_dim > dims->d || rope->rot_dim % 16) return VP_ERR_UNSUPPORTED_SHAPE;
   if (rope->rot_dim && !rope->turns) return VP_ERR_INVALID_ARG;
   if ((rope->interleaved != 0 && rope->interleaved != 1) || !isfinite(rope->scale))
     return VP_ERR_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(rope->turns) & 7u) return VP_ERR_ALIGNMENT;
+  if (T == 0) return VP_OK;  // empty tensors have no address
+  if (!cu || !q != !q_out) return VP_ERR_INVALID_ARG;
   if (q) {
     VP_TRY(check_rows(q, q_stride, dims->Hq, dims->d));
     VP_TRY(check_rows(q_out, q_out_stride, dims->Hq, dims->d));
@@ -154,7 +156,6 @@ vp_status vp_rope_append(const vp_attn_dims* dims, const vp_rope_options* rope, 
   if ((q && q == q_out && q_stride != q_out_stride) || (k == k_out && k_stride != k_out_stride))
     return VP_ERR_INVALID_ARG;
   if (ws && ws_bytes < 256) return VP_ERR_WORKSPACE;
-  if (T == 0) return VP_OK;
   if (!device_is_sm103()) return VP_ERR_UNSUPPORTED_DEVICE;
   RopeAppendArgs a{};
   a.T = T;
@@ -191,6 +192,7 @@ vp_status vp_prompt_attention(const vp_attn_dims* dims, int32_t T, int32_t B, co
                               float* lse, void* ws, size_t ws_bytes, void* stream) {
   VP_TRY(check_attn_dims(dims));
   VP_TRY(check_counts(T, B));
+  if (T == 0) return VP_OK;
   if (!cu) return VP_ERR_INVALID_ARG;
   VP_TRY(check_rows(q, q_stride, dims->Hq, dims->d));
   VP_TRY(check_rows(k, k_stride, dims->Hkv, dims->d));
@@ -198,7 +200,6 @@ vp_status vp_prompt_attention(const vp_attn_dims* dims, int32_t T, int32_t B, co
   VP_TRY(check_rows(out, out_stride, dims->Hq, dims->d));
   if (!ws || ws_bytes < seq_scratch_bytes(dims->d)) return VP_ERR_WORKSPACE;
   if (!aligned16(ws)) return VP_ERR_ALIGNMENT;
-  if (T == 0) return VP_OK;
   if (!device_is_sm103()) return VP_ERR_UNSUPPORTED_DEVICE;
   SeqAttnArgs a = make_args(dims, T, B, q, q_stride, cu, out, out_stride, lse, ws);
   a.k = static_cast<const uint16_t*>(k);
@@ -215,13 +216,13 @@ vp_status vp_paged_attention(const vp_attn_dims* dims, int32_t T, int32_t B, con
                              void* ws, size_t ws_bytes, void* stream) {
   VP_TRY(check_attn_dims(dims));
   VP_TRY(check_counts(T, B));
+  if (T == 0) return VP_OK;
   if (!cu || !kv_len) return VP_ERR_INVALID_ARG;
   VP_TRY(check_rows(q, q_stride, dims->Hq, dims->d));
   VP_TRY(check_rows(out, out_stride, dims->Hq, dims->d));
   VP_TRY(check_kv(kv));
   if (!ws || ws_bytes < seq_scratch_bytes(dims->d)) return VP_ERR_WORKSPACE;
   if (!aligned16(ws)) return VP_ERR_ALIGNMENT;
-  if (T == 0) return VP_OK;
   if (!device_is_sm103()) return VP_ERR_UNSUPPORTED_DEVICE;
   SeqAttnArgs a = make_args(dims, T, B, q, q_stride, cu, out, out_stride, lse, ws);
   a.kv_len = kv_len;

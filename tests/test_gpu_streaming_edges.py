@@ -1,5 +1,5 @@
 """Streaming attention on the GPU where its kernels' schedules and number ranges end: items cut between
-CTAs, large scores, against the 64-bit definitions (oracle.streaming)."""
+CTAs, large scores, no tokens, against the 64-bit definitions (oracle.streaming)."""
 import math
 
 import numpy as np
@@ -110,3 +110,42 @@ def test_scores_from_small_to_far(n, d, dtype, top, scale, sign, order):
     if order == "mixed":
         x = x[torch.randperm(n, generator=torch.Generator().manual_seed(n))]
     _large_scores([x], [top[0]], n, d, dtype, scale, sign)
+
+
+# ------------------------------------------------------------------------------ no tokens
+def test_calls_without_new_tokens():
+    """No new tokens (empty tensors have no address): nothing is done, and nothing refused."""
+    c = Cache(3, [70, 5], 2, 64, 16, BF)
+    dims = vpb.attn_dims(4, 2, 64)
+    q, k = torch.empty(0, 4, 64, dtype=BF, device="cuda"), torch.empty(0, 2, 64, dtype=BF, device="cuda")
+    assert q.data_ptr() == 0
+    lse = torch.empty(0, 4, device="cuda")
+    rope = vpb.rope_options(vpb.rope_turns(64).cuda())
+    ws = vpb.attn_workspace(dims, 0, 2)
+    k0, v0 = c.k.clone(), c.v.clone()
+    for cu, kv_len in ((_cu([0, 0]), c.kv_len), (_cu([]), c.kv_len[:0])):
+        vpb.vp_rope_append(dims, rope, q, k, k, cu, kv_len, None, c.kv, q_out=q, k_out=k, ws=ws)
+        vpb.vp_prompt_attention(dims, q, k, k, cu, q, lse, ws)
+        vpb.vp_paged_attention(dims, q, cu, kv_len, c.kv, q, lse, ws)
+    assert vpb.vp_read_device_error(ws) == 0
+
+    def same(a, b):  # NaN in unused slots
+        return torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+    assert same(c.k, k0) and same(c.v, v0)
+
+
+def test_view_stream_example_without_new_tokens():
+    import examples.stream_views as ex
+
+    g = torch.Generator(device="cuda").manual_seed(3)
+    blocks = [ex.make_block(g, 256, 4, 2)]
+    s = ex.ViewStream(blocks, 2, 20, hq=4, hkv=2)
+    x = torch.randn(9, 256, generator=g, device="cuda").to(BF)
+    assert s.extend(x[:0], [0, 0]).shape == (0, 256) and s.held == [0, 0]
+    a = s.extend(x[:6], [4, 2])
+    assert s.query(x[:0], [0, 0]).shape == (0, 256) and s.extend(x[:0], [0, 0]).shape == (0, 256)
+    assert s.held == [4, 2] and s.errors() == 0
+    b = s.extend(x[6:], [3, 0])
+    t = ex.ViewStream(blocks, 2, 20, hq=4, hkv=2)
+    assert torch.equal(t.extend(x[:6], [4, 2]), a) and torch.equal(t.extend(x[6:], [3, 0]), b)
