@@ -370,7 +370,8 @@ vp_status vp_router_noalloc_error(uint32_t* host_bits, void* stream);
  *
  * Strides are in elements between tokens (a multiple of 8, at least heads x d), so that q, k and v
  * may be slices of a packed projection [T][Hq + 2 Hkv][d]; heads and channels are contiguous.
- * Every tensor pointer is 16-byte aligned; with T = 0 none is looked at and nothing is done.
+ * Every tensor pointer is 16-byte aligned (cu, kv_len, positions, lse and page_table, which may be
+ * slices, 4); with T = 0 none is looked at and nothing is done.
  * Lengths, offsets and the page table are read on the device when the kernels run; a length or page
  * id outside the cache is clamped or skipped and sets VP_DEVERR_PAGE in the workspace's error
  * word.

@@ -20,6 +20,8 @@ constexpr int32_t kMaxTokens = 1 << 30;
   } while (0)
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+// Of 32-bit values read one by one, which may be slices of longer arrays.
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 vp_status check_attn_dims(const vp_attn_dims* dm) {
   if (!dm) return VP_ERR_INVALID_ARG;
@@ -47,7 +49,7 @@ vp_status check_rows(const void* p, int64_t stride, int heads, int d) {
 
 vp_status check_kv(const vp_paged_kv* kv) {
   if (!kv || !kv->k || !kv->v || !kv->page_table) return VP_ERR_INVALID_ARG;
-  if (!aligned16(kv->k) || !aligned16(kv->v)) return VP_ERR_ALIGNMENT;
+  if (!aligned16(kv->k) || !aligned16(kv->v) || !aligned4(kv->page_table)) return VP_ERR_ALIGNMENT;
   const int ps = kv->page_size;
   if (ps < 16 || ps > 1024 || (ps & (ps - 1)) || kv->n_pages < 1 || kv->table_width < 1)
     return VP_ERR_UNSUPPORTED_SHAPE;
@@ -139,6 +141,7 @@ vp_status vp_rope_append(const vp_attn_dims* dims, const vp_rope_options* rope, 
   if (reinterpret_cast<uintptr_t>(rope->turns) & 7u) return VP_ERR_ALIGNMENT;
   if (T == 0) return VP_OK;  // empty tensors have no address
   if (!cu || !q != !q_out) return VP_ERR_INVALID_ARG;
+  if (!aligned4(cu) || !aligned4(kv_len) || !aligned4(positions)) return VP_ERR_ALIGNMENT;
   if (q) {
     VP_TRY(check_rows(q, q_stride, dims->Hq, dims->d));
     VP_TRY(check_rows(q_out, q_out_stride, dims->Hq, dims->d));
@@ -156,6 +159,7 @@ vp_status vp_rope_append(const vp_attn_dims* dims, const vp_rope_options* rope, 
   if ((q && q == q_out && q_stride != q_out_stride) || (k == k_out && k_stride != k_out_stride))
     return VP_ERR_INVALID_ARG;
   if (ws && ws_bytes < 256) return VP_ERR_WORKSPACE;
+  if (!aligned16(ws)) return VP_ERR_ALIGNMENT;
   if (!device_is_sm103()) return VP_ERR_UNSUPPORTED_DEVICE;
   RopeAppendArgs a{};
   a.T = T;
@@ -194,6 +198,7 @@ vp_status vp_prompt_attention(const vp_attn_dims* dims, int32_t T, int32_t B, co
   VP_TRY(check_counts(T, B));
   if (T == 0) return VP_OK;
   if (!cu) return VP_ERR_INVALID_ARG;
+  if (!aligned4(cu) || !aligned4(lse)) return VP_ERR_ALIGNMENT;
   VP_TRY(check_rows(q, q_stride, dims->Hq, dims->d));
   VP_TRY(check_rows(k, k_stride, dims->Hkv, dims->d));
   VP_TRY(check_rows(v, v_stride, dims->Hkv, dims->d));
@@ -218,6 +223,7 @@ vp_status vp_paged_attention(const vp_attn_dims* dims, int32_t T, int32_t B, con
   VP_TRY(check_counts(T, B));
   if (T == 0) return VP_OK;
   if (!cu || !kv_len) return VP_ERR_INVALID_ARG;
+  if (!aligned4(cu) || !aligned4(kv_len) || !aligned4(lse)) return VP_ERR_ALIGNMENT;
   VP_TRY(check_rows(q, q_stride, dims->Hq, dims->d));
   VP_TRY(check_rows(out, out_stride, dims->Hq, dims->d));
   VP_TRY(check_kv(kv));
