@@ -1,5 +1,6 @@
 """Streaming attention on the GPU where its kernels' schedules and number ranges end: items cut between
-CTAs, large scores, no tokens, against the 64-bit definitions (oracle.streaming)."""
+CTAs, chains that start anew at mask blocks, large scores, no tokens, against the 64-bit definitions
+(oracle.streaming).  Cases that are meant for one of the two kernels check that it ran."""
 import math
 
 import numpy as np
@@ -149,3 +150,139 @@ def test_view_stream_example_without_new_tokens():
     b = s.extend(x[6:], [3, 0])
     t = ex.ViewStream(blocks, 2, 20, hq=4, hkv=2)
     assert torch.equal(t.extend(x[:6], [4, 2]), a) and torch.equal(t.extend(x[6:], [3, 0]), b)
+
+
+# ------------------------------------------------------------------------------ which kernel
+def _ran(ws):
+    """(kernel, number of cut items) of the last call that was given `ws`, filled with ones before it.  Each
+    CTA leaves 32 bytes in the list behind the error word: a CTA per SM is the tile kernel, more of them
+    the kernel for few rows.  An entry's first value is the number of an item's parts."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    recs = ws[256:256 + 32 * 2 * sms].view(torch.int32).view(2 * sms, 8)[:, 0].cpu()
+    tiles = bool((recs[sms:] == -1).all())
+    assert (recs[:sms] >= 0).all()
+    return ("tiles" if tiles else "rows"), int((recs[:sms] > 0).sum())
+
+
+def _chains_start_anew(group, block):
+    """Whether a chain of 128 / group tokens starts at every mask block (at most 1/16 of its rows empty)."""
+    n = 128 // group
+    return block > n and 16 * (-block % n) <= block
+
+
+def _lse_and_out(T, hq, d, dtype):
+    return (torch.full((T, hq), float("nan"), device="cuda"),
+            torch.full((T, hq, d), float("nan"), dtype=dtype, device="cuda"))
+
+
+# ------------------------------------------------------------------------------ chains at mask blocks
+@pytest.mark.parametrize("lens,hq,hkv,d,block,dtype,cut", [
+    ([2948], 2, 2, 64, 1374, BF, True),                # two views and part of a third, 11 chains a view
+    ([1374, 0, 130, 1, 2748], 4, 1, 64, 1374, FP, True),  # 43 chains a view
+    ([2061], 8, 2, 128, 1374, BF, True),
+    ([1374, 2061, 77], 3, 3, 128, 1374, FP, True),
+    ([1100, 128, 129], 16, 4, 64, 128, BF, True),      # blocks of whole chains
+    ([2100, 127, 254], 12, 6, 64, 127, FP, True),
+    ([1500, 125], 6, 2, 128, 125, BF, True),           # chains of 42 tokens
+    ([777, 250, 251, 749], 16, 16, 128, 250, FP, False),
+    ([261, 522, 300], 8, 8, 64, 250, BF, False),
+    ([5000], 1, 1, 64, 250, FP, True),
+])
+def test_prompt_chains_at_mask_blocks(lens, hq, hkv, d, block, dtype, cut):
+    assert _chains_start_anew(hq // hkv, block)
+    T, B = sum(lens), len(lens)
+    dims = vpb.attn_dims(hq, hkv, d, dtype=dtype, block=block)
+    qkv = _randn(41, T, hq + 2 * hkv, d, dtype=dtype)
+    q, k, v = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
+    ws = _dirty_ws(dims, T, B)
+    lse, out = _lse_and_out(T, hq, d, dtype)
+    vpb.vp_prompt_attention(dims, q, k, v, _cu(lens), out, lse, ws)
+    assert vpb.vp_read_device_error(ws) == 0
+    kernel, cuts = _ran(ws)
+    assert kernel == "tiles" and (cuts > 0) == cut
+    t = 0
+    for n in lens:
+        r = slice(t, t + n)
+        if n:
+            want = so.seq_attention(_f64(q[r]), _f64(k[r]), _f64(v[r]), so.row_limits(n, n, block), 1 / math.sqrt(d))
+            _check_attention(_f64(out[r]), _f64(lse[r]), want, dtype, n, float(v.abs().max()))
+        t += n
+
+
+@pytest.mark.parametrize("ql,kl,hq,hkv,d,page,block,dtype,cut", [
+    ([1374], [4122], 4, 4, 64, 64, 1374, BF, True),           # a view over two
+    ([1500, 1374], [2874, 4000], 8, 2, 64, 16, 1374, FP, True),   # a chunk that ends inside a view
+    ([2748], [2748], 4, 1, 128, 128, 1374, BF, True),
+    ([1374, 200], [3000, 9000], 2, 2, 128, 32, 1374, FP, True),
+    ([300, 0, 500, 128], [1300, 70, 500, 2000], 8, 2, 64, 64, 128, BF, True),
+    ([500, 251], [400, 3000], 4, 4, 128, 16, 250, FP, True),  # more new tokens than the sequence holds
+    ([400, 375], [2000, 375], 6, 2, 64, 256, 125, FP, True),
+])
+def test_paged_chains_at_mask_blocks(ql, kl, hq, hkv, d, page, block, dtype, cut):
+    assert _chains_start_anew(hq // hkv, block)
+    _paged_case(ql, kl, hq, hkv, d, page, block, dtype, "tiles", cut)
+
+
+def _paged_case(ql, kl, hq, hkv, d, page, block, dtype, kernel, cut):
+    T, B = sum(ql), len(ql)
+    dims = vpb.attn_dims(hq, hkv, d, dtype=dtype, block=block)
+    c = Cache(42, kl, hkv, d, page, dtype)
+    q = _randn(43, T, hq, d, dtype=dtype)
+    ws = _dirty_ws(dims, T, B)
+    lse, out = _lse_and_out(T, hq, d, dtype)
+    vpb.vp_paged_attention(dims, q, _cu(ql), c.kv_len, c.kv, out, lse, ws)
+    assert vpb.vp_read_device_error(ws) == 0
+    ran, cuts = _ran(ws)
+    assert ran == kernel and (cuts > 0) == cut
+    t = 0
+    for b, (m, n) in enumerate(zip(ql, kl)):
+        kd, vd = c.dense[b]
+        lim = so.row_limits(m, n, block)
+        if m:
+            want = so.seq_attention(_f64(q[t:t + m]), _f64(kd), _f64(vd), lim, 1 / math.sqrt(d))
+            _check_attention(_f64(out[t:t + m]), _f64(lse[t:t + m]), want, dtype, n, float(vd.abs().max()) if n else 0.0)
+            assert (out[t:t + m][torch.from_numpy(lim <= 0).cuda()] == 0).all()
+        t += m
+
+
+# ------------------------------------------------------------------------------ every instance of both kernels
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("ql,kl,block,kernel,cut", [
+    ([500], [6001], 1, "tiles", True),
+    ([300, 261, 0, 700], [300, 3000, 9, 701], 1, "tiles", True),
+    ([600], [4000], 0, "tiles", True),
+    ([400, 300], [250, 310], 1, "tiles", False),   # the first has rows that see nothing
+    ([1, 1, 1], [3000, 1, 777], 1, "rows", True),
+    ([5, 2], [2049, 4000], 1, "rows", True),
+    ([3], [9000], 0, "rows", True),
+])
+def test_paged_instances(ql, kl, block, kernel, cut, d, dtype):
+    _paged_case(ql, kl, 8, 2, d, 32, block, dtype, kernel, cut)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("lens,hkv,block,kernel,cut", [
+    ([3001], 2, 1, "tiles", True),
+    ([1800, 33, 900], 2, 0, "tiles", True),
+    ([2500], 1, 7, "tiles", True),
+    ([3, 400, 3], 1, 1, "rows", True),
+])
+def test_prompt_instances(lens, hkv, block, kernel, cut, d, dtype):
+    T, hq = sum(lens), 4 * hkv
+    dims = vpb.attn_dims(hq, hkv, d, dtype=dtype, block=block)
+    qkv = _randn(44, T, hq + 2 * hkv, d, dtype=dtype)
+    q, k, v = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
+    ws = _dirty_ws(dims, T, len(lens))
+    lse, out = _lse_and_out(T, hq, d, dtype)
+    vpb.vp_prompt_attention(dims, q, k, v, _cu(lens), out, lse, ws)
+    assert vpb.vp_read_device_error(ws) == 0
+    ran, cuts = _ran(ws)
+    assert ran == kernel and (cuts > 0) == cut
+    t = 0
+    for n in lens:
+        r = slice(t, t + n)
+        want = so.seq_attention(_f64(q[r]), _f64(k[r]), _f64(v[r]), so.row_limits(n, n, block), 1 / math.sqrt(d))
+        _check_attention(_f64(out[r]), _f64(lse[r]), want, dtype, n, float(v.abs().max()))
+        t += n
