@@ -286,3 +286,71 @@ def test_prompt_instances(lens, hkv, block, kernel, cut, d, dtype):
         want = so.seq_attention(_f64(q[r]), _f64(k[r]), _f64(v[r]), so.row_limits(n, n, block), 1 / math.sqrt(d))
         _check_attention(_f64(out[r]), _f64(lse[r]), want, dtype, n, float(v.abs().max()))
         t += n
+
+
+# ------------------------------------------------------------------------------ the place of every value
+def _marked_v(n, d, dtype):
+    """V [n][1][d] that is 0 but in channel (j / 16) mod d, whose size tells the laps of 16 d keys apart: what
+    comes out in a channel is the weight of its keys, so a tile or page taken from elsewhere shows."""
+    v = torch.zeros(n, 1, d)
+    part = torch.arange(n) // 16
+    v[torch.arange(n), 0, part % d] = 200.0 + 24.0 * (part // d % 32).float()
+    return v.to(dtype).cuda()  # at most 944: exact in 8 bits (multiples of 8 up to 2^10: bf16 holds multiples of 4)
+
+
+def _check_marked(got, q, k, v, lim, d, dtype):
+    """Tolerances.  Output and weights rounded to the storage type: eps (spread + |out|).  Scores in 32 bits:
+    2^-11 spread, as for all inputs of unit normal channels.  fp16 weights are held 2^7 above their value
+    relative to a reference at most 2^8 below the row's maximum, so the row's weights sum to 2^7 and more (2^-5
+    of that allowed for the reference's own rounding), and one below 2^-14 is off by up to 2^-25:
+    n 2^-32 max |v| (1 + 2^-5)."""
+    eps = {BF: 2.0 ** -8, FP: 2.0 ** -11}[dtype]
+    out, _, spread = so.seq_attention(q, k, v, lim, 1 / math.sqrt(d))
+    tol = eps * (spread + np.abs(out)) + 2.0 ** -11 * spread + 2.0 ** -24
+    if dtype == FP:
+        tol = tol + np.asarray(lim).reshape(-1, 1, 1) * 2.0 ** -32 * 944 * (1 + 2.0 ** -5)
+    err = np.abs(got - out)
+    assert np.all(err <= tol), f"worst ratio {np.max(err / tol):.3f}"
+
+
+@pytest.mark.parametrize("n,L,hq,page,kernel", [
+    (1, 30011, 8, 1024, "rows"),
+    (1, 20000, 16, 16, "rows"),
+    (3, 12345, 4, 64, "rows"),
+    (300, 9001, 2, 16, "tiles"),
+    (200, 30011, 4, 128, "tiles"),
+    (129, 70001, 2, 32, "tiles"),
+])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [FP, BF])
+def test_paged_values_are_those_of_their_keys(n, L, hq, page, kernel, d, dtype):
+    dims = vpb.attn_dims(hq, 1, d, dtype=dtype)
+    c = Cache(51, [L], 1, d, page, dtype)
+    kd, vd = c.dense[0][0], _marked_v(L, d, dtype)
+    c.write(0, kd, vd)
+    q, ws = _randn(52, n, hq, d, dtype=dtype), _dirty_ws(dims, n, 1)
+    out = torch.full_like(q, float("nan"))
+    vpb.vp_paged_attention(dims, q, _cu([n]), c.kv_len, c.kv, out, None, ws)
+    assert vpb.vp_read_device_error(ws) == 0 and _ran(ws)[0] == kernel
+    rows = sorted({0, n // 3, n - 1})  # of a chunk, three tokens
+    _check_marked(_f64(out[rows]), _f64(q[rows]), _f64(kd), _f64(vd), so.row_limits(n, L, 1)[rows], d, dtype)
+
+
+@pytest.mark.parametrize("lens,hq,block,kernel", [([9001], 1, 1, "tiles"), ([700, 5000], 2, 0, "tiles"),
+                                                  ([3, 600, 3], 2, 1, "rows")])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [FP, BF])
+def test_prompt_values_are_those_of_their_keys(lens, hq, block, kernel, d, dtype):
+    T = sum(lens)
+    dims = vpb.attn_dims(hq, 1, d, dtype=dtype, block=block)
+    q, k, v = _randn(53, T, hq, d, dtype=dtype), _randn(54, T, 1, d, dtype=dtype), _marked_v(T, d, dtype)
+    ws, out = _dirty_ws(dims, T, len(lens)), torch.full_like(q, float("nan"))
+    vpb.vp_prompt_attention(dims, q, k, v, _cu(lens), out, None, ws)
+    assert vpb.vp_read_device_error(ws) == 0 and _ran(ws)[0] == kernel
+    t = 0
+    for n in lens:
+        rows = sorted({0, n // 2, n - 1})
+        at = [t + r for r in rows]
+        _check_marked(_f64(out[at]), _f64(q[at]), _f64(k[t:t + n]), _f64(v[t:t + n]), so.row_limits(n, n, block)[rows],
+                      d, dtype)
+        t += n
