@@ -9,8 +9,9 @@
 // sine is taken once per token and frequency and not once per head, then move 32 bytes (two 16-byte
 // vectors: the two halves of eight pairs, or sixteen neighbouring channels) per step, kRaUnroll
 // steps' loads in flight per thread.  Measured on GB300: 43,968 tokens, 16 q heads and 8 kv heads of
-// 128, 110.6 us (6.5 TB/s, 0.96 of the measured copy bandwidth; 1, 3, 4 steps in flight: 117, 112,
-// 116 us; 4 or 16 tokens per CTA instead of 8: 126, 113 us); 64 single tokens of 24 heads of 64: 3.5 us.
+// 128, 110.6 us on the device (6.5 TB/s, 0.96 of the measured copy bandwidth; 1, 3, 4 steps in flight: 117,
+// 112, 116 us; 4 or 16 tokens per CTA instead of 8: 126, 113 us), 111.6 us as called; 64 single tokens of 24
+// heads of 64: 3.6 us on the device.
 #include "common.cuh"
 #include "seq.h"
 

@@ -35,11 +35,12 @@
 // tensor core needs (A and B of one MMA have one type).  Every wait is bounded; a CTA that gives up
 // lets its copies and MMAs land.
 //
-// Bounds: 4 d flop and one exponential per row and visible key.  Measured on GB300: 43,968 causal
-// tokens, 16 heads of 64 on 4 kv heads, 2.94 ms (1,350 TFLOP/s, 0.71 of the burst bf16 peak; the
-// exponentials and the latency of a chain's steps bound d 64); 32,768 tokens, 16 heads of 128, no mask,
-// 5.6 ms (1,570 TFLOP/s, 0.83 of burst; the tensor pipe).  Between two items of a CTA lie about
-// 7,000 clocks of drain, epilogue and fill (3.7 us), which is what short prompts pay.
+// Bounds: 4 d flop and one exponential per row and visible key.  Measured on GB300, as called: 43,968
+// causal tokens, 16 heads of 64 on 4 kv heads, 3.01 ms (1,315 TFLOP/s, 0.70 of the burst bf16 peak; the
+// latency of a chain's steps bounds d 64, the exponentials' pipe is busy 47 % of the time); 32,768
+// tokens, 16 heads of 128, no mask, 5.5 ms in bf16 (1,600 TFLOP/s, 0.85 of burst; the tensor pipe), 6.0 ms
+// in fp16.  Between two items of a CTA lie about 7,000 clocks of drain, epilogue and fill (3.7 us),
+// which is what short prompts pay.
 #include <float.h>
 #include <math.h>
 

@@ -18,8 +18,8 @@
 //               the four warps' results are joined at the end of an item.
 // Scores, maxima, sums and outputs are held in 32 bits; P is rounded to the storage type.
 // Measured on GB300: 4 single tokens over 130,003 to 137,400 keys, 32 heads of 128 on 4 kv heads, pages
-// of 16: 166 us (6.6 TB/s, 0.98 of the measured copy bandwidth); 64 tokens over 97 to 16,381 keys, 16
-// heads of 64 on 4: 40.6 us (5.3 TB/s; the first 2.6 us find the place, the last 4 join the parts).
+// of 16: 169 us as called (6.5 TB/s, 0.95 of the measured copy bandwidth); 64 tokens over 97 to 16,381 keys,
+// 16 heads of 64 on 4: 41.7 us (5.1 TB/s; the first 2.6 us find the place, the last 4 join the parts).
 // V values that are not finite and not seen by every row are taken out of the tile (0 x inf
 // would reach all rows) and added to the rows that see them.
 #include <float.h>
@@ -39,7 +39,7 @@ constexpr float kUnset = -FLT_MAX;
 constexpr float kRescaleThreshold = 8.f;  // log2 units
 // An item costs about as much as this many units on top of its own (its rows' q, the join of the warps):
 // the extent of an item is kItemCost + its units, and cuts within the first kItemCost move to its start.
-// (64 single tokens over 97 to 16,381 keys: 47.4 us without, 43.0 with 1, 40.6 with 2 to 5.)
+// (64 single tokens over 97 to 16,381 keys, on the device: 47.4 us without, 43.0 with 1, 40.6 with 2 to 5.)
 constexpr int kItemCost = 4;
 // The same where items are kept whole and there are no more of them than CTAs: runs of one item, so that
 // none has two while another has none (prompts of 1, 16, 261, 4 and 65 tokens, 16 heads of 64: 10.8 ->
