@@ -354,3 +354,28 @@ def test_prompt_values_are_those_of_their_keys(lens, hq, block, kernel, d, dtype
         _check_marked(_f64(out[at]), _f64(q[at]), _f64(k[t:t + n]), _f64(v[t:t + n]), so.row_limits(n, n, block)[rows],
                       d, dtype)
         t += n
+
+
+# ------------------------------------------------------------------------------ wide page tables
+@pytest.mark.parametrize("ql,kl", [([1] * 20, [13 * i % 300 + 1 for i in range(20)]), ([70, 1, 33], [300, 200, 33]),
+                                   ([1] * 63 + [449], [7 * i % 290 + 1 for i in range(63)] + [3000])])
+@pytest.mark.parametrize("d,dtype", [(64, BF), (128, FP)])
+def test_tables_wider_than_their_sequences(ql, kl, d, dtype):
+    """A table for 131,072 tokens a sequence that hold few, its other entries on no page; single tokens and
+    a chunk in one call."""
+    T, B, hq, hkv, page = sum(ql), len(ql), 8, 2, 64
+    dims = vpb.attn_dims(hq, hkv, d, dtype=dtype)
+    c = Cache(61, kl, hkv, d, page, dtype)
+    table = torch.full((B, 131072 // page), -1, dtype=torch.int32, device="cuda")
+    table[:, :c.table.shape[1]] = c.table
+    kv = vpb.paged_kv(c.k, c.v, table)
+    q, ws = _randn(62, T, hq, d, dtype=dtype), _dirty_ws(dims, T, B)
+    lse, out = _lse_and_out(T, hq, d, dtype)
+    vpb.vp_paged_attention(dims, q, _cu(ql), c.kv_len, kv, out, lse, ws)
+    assert vpb.vp_read_device_error(ws) == 0
+    t = 0
+    for b, (m, n) in enumerate(zip(ql, kl)):
+        kd, vd = c.dense[b]
+        want = so.seq_attention(_f64(q[t:t + m]), _f64(kd), _f64(vd), so.row_limits(m, n, 1), 1 / math.sqrt(d))
+        _check_attention(_f64(out[t:t + m]), _f64(lse[t:t + m]), want, dtype, n, float(vd.abs().max()))
+        t += m
