@@ -46,7 +46,7 @@ struct Rows8Smem {
   uint8_t v[C::kStages][kBN * D];
   uint8_t k_scale[C::kStages][kBN];
   uint8_t v_scale[C::kStages][kBN];
-  struct Scales {  // of a warp's keys: K's times the scores' scale, V's as fp16
+  struct Scales {  // of a warp's keys: K's, V's as fp16
     float k[32];
     uint16_t v[32];
   } scales[kWarps];
@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(kThreads, Rows8Cfg<D, kRows>::kPerSm)
       // The keys' scales, a key per lane; NaN where there is none.
       {
         const uint32_t ke = sm.k_scale[st][32 * warp + lane];
-        scales.k[lane] = prm.scale_log2 * __uint_as_float(bad_scale(ke) ? 0x7FC00000u : ke << 23);
+        scales.k[lane] = __uint_as_float(bad_scale(ke) ? 0x7FC00000u : ke << 23);
         scales.v[lane] = (uint16_t)scale_half(sm.v_scale[st][32 * warp + lane]);
         __syncwarp();
       }
@@ -382,9 +382,11 @@ __global__ void __launch_bounds__(kThreads, Rows8Cfg<D, kRows>::kPerSm)
           for (int b = 0; b < kNB; ++b)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
+              // q . k first, by powers of two, then the scale: their product ahead of it may be past 32 bits
+              // where the score is not (0 x inf; q of 2^-125 under a scale of 2^125).
               float& x = c[b][g][2 * k + i];
-              x *= f;
-              if (!F16) x *= back[b][i];
+              x *= F16 ? f : f * back[b][i];
+              x *= prm.scale_log2;
               if (masked && key0 + 16 * g + 8 * k + r0 >= lim[b][i]) x = -INFINITY;
               mx[b][i] = fmaxf(mx[b][i], x);
             }
