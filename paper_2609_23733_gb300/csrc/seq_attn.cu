@@ -1166,7 +1166,8 @@ __global__ void __launch_bounds__(Cfg<D, kKeys == Keys::paged8>::kThreads, 1)
           mx = fmaxf(fmax3(t[0], t[1], t[2]), fmax3(t[3], t[4], fmax3(t[5], t[6], t[7])));
         }
         float mul = fabsf(kQHalf ? mx * back : mx) < prm.far_from ? cs : prm.far_scale;
-        if (kQHalf) mul = fmaxf(mul * back, kLeastScale);
+        // (Held to finite values: q . k may be 0 under a factor past 32 bits.)
+        if (kQHalf) mul = fminf(fmaxf(mul * back, kLeastScale), FLT_MAX);
         const float to = reference_point<kHalf>(mx, mul);
         float alpha = 1.f;
         bool need = false;
