@@ -5,6 +5,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <float.h>
 #include <stdint.h>
 
 #include "common.cuh"
@@ -204,7 +205,9 @@ cudaError_t make_tmap_8bit_4d(CUtensorMap* map, const void* base, const uint64_t
 // m = mx far_scale is exact.  Two different scores lie at least 16 apart there, so a weight w < 1 is below
 // 2^-16 and comes out between w^2 and w.  The log-sum is put back into units of cs.
 constexpr float kFarScore = 1 << 28;
-constexpr float kLeastScale = 1e-30f;  // of the tile kernel's |cs|, so that a hidden score, -inf, stays -inf
+// Of the tile kernel's |cs|, so that a hidden score, -inf, stays -inf; the least there is, since scores (of bf16) may be
+// as large as cs is small.
+constexpr float kLeastScale = FLT_TRUE_MIN;
 // m in units of cs: a near tile's m is below kFarScore (far_from is a little below kFarScore / cs), a far
 // one's that is below it too has far_unit = 1 to 2^-19.
 __device__ __forceinline__ float near_units(const SeqAttnArgs& a, float m) {

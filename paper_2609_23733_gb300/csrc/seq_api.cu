@@ -1,5 +1,6 @@
 // C entry points of the streaming operators (include/vp.h): argument checks and launches.
 #include <cuda_runtime.h>
+#include <float.h>
 #include <math.h>
 
 #include "internal.h"
@@ -155,7 +156,7 @@ SeqAttnArgs make_args(const vp_attn_dims* dm, int32_t T, int32_t B, const void* 
   const bool power = frexpf(cs, &e) == 0.5f;  // cs in [2^(e - 1), 2^e)
   a.far_scale = power ? cs : ldexpf(1.f, e < 127 ? e : 127);
   a.far_unit = cs / a.far_scale;
-  a.far_from = (float)(kFarScore * (1. - 0x1p-20) / cs);
+  a.far_from = (float)fmin(kFarScore * (1. - 0x1p-20) / cs, FLT_MAX);  // below 2^-100 no finite score is far
   a.q = static_cast<const uint16_t*>(q);
   a.q_stride = q_stride;
   a.cu = cu;

@@ -65,7 +65,8 @@ SHAPES = [(1, 2, "rows"), (5, 4, "rows"), (600, 12, "tiles")]
 # ------------------------------------------------------------------------------ factors of scores
 @pytest.mark.parametrize("n,hq,kernel", SHAPES)
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("power,scale", [(-110, 2.0 ** 110), (-125, 1.75 * 2.0 ** 125), (110, 2.0 ** -99), (-20, 1.1 * 2.0 ** 18)])
+@pytest.mark.parametrize("power,scale", [(-110, 2.0 ** 110), (-125, 1.75 * 2.0 ** 125), (110, 2.0 ** -99), (120, 2.0 ** -119), (120, 0.0),
+                                         (-20, 1.1 * 2.0 ** 18)])
 def test_scores_whose_factors_are_far_apart(n, hq, kernel, d, power, scale):
     """bf16 rows of q of any size under a scale that brings the scores back to the unit: the weights are those of the
     scores, whatever the products of some of their factors would be."""
