@@ -1,5 +1,6 @@
 """The 8-bit cache's operators at the ends of their number ranges, against the 64-bit definitions (oracle.streaming):
-factors of scores whose products leave 32 bits.
+infinities and NaN in q and under a norm, factors of scores whose products leave 32 bits, values at the smallest and
+largest scales.
 
 Tolerances of attention, where test_gpu_cache8.py allows more than a key can be off.  Weights are fp16 numbers,
 the row's largest at least 2^7 (the reference point lies 2^7 below the running maximum, or lower), so a weight p
@@ -62,6 +63,85 @@ def _exact(seed, L, d):
 SHAPES = [(1, 2, "rows"), (5, 4, "rows"), (600, 12, "tiles")]
 
 
+# ------------------------------------------------------------------------------ infinities and NaN
+@pytest.mark.parametrize("n,hq,kernel", SHAPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_rows_of_q_that_are_not_finite(n, hq, kernel, d, dtype):
+    """A row of q with an infinity or a NaN gives NaN; the rows beside it are those of the definition.  (Every key
+    with an infinite score of one sign: its softmax has no value either.)"""
+    L = 1500
+    k, v = _exact(1, L, d), _exact(2, L, d)
+    assert (k[:, 0, 3] == 0).sum() < L // 2
+    q = _f64(_randn(3, n, hq, d, dtype=dtype))
+    bad = np.zeros((n, hq), bool)
+    bad[0, 0] = bad[n // 2, hq - 1] = bad[n - 1, hq // 2] = True
+    for value in (np.nan, np.inf, -np.inf):
+        x = q.copy()
+        x[bad, 3] = value
+        out, lse = _run(x, k, v, dtype, 0.125, kernel)
+        assert np.isnan(out[bad]).all() and not np.isfinite(lse[bad]).any()
+        rows = sorted({0, n // 2, n - 1, n // 3})
+        want, want_lse, tol = _tolerance(q[rows], k, v, so.row_limits(n, L, 1)[rows], 0.125, dtype)
+        good = ~bad[rows]
+        assert np.all(np.abs(out[rows] - want)[good] <= tol[good])
+        assert np.all(np.abs(lse[rows] - want_lse)[good] <= 4e-5 + 4e-6 * np.abs(want_lse[good]))
+        assert np.isfinite(out[~bad]).all() and np.isfinite(lse[~bad]).all()
+
+
+@pytest.mark.parametrize("n,kernel", [(6, "rows"), (900, "tiles")])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_rows_that_see_nothing_have_zeros_whatever_q_holds(n, kernel, dtype):
+    L = 4 if n == 6 else 700
+    q = _f64(_randn(3, n, 8, 64, dtype=dtype))
+    empty = so.row_limits(n, L, 1) <= 0
+    assert empty.sum() == n - L
+    q[0], q[1, :, 5] = np.nan, np.inf
+    out, lse = _run(q, _exact(1, L, 64), _exact(2, L, 64), dtype, 0.125, kernel)
+    assert (out[empty] == 0).all() and np.isneginf(lse[empty]).all() and np.isfinite(out[~empty]).all()
+
+
+@pytest.mark.parametrize("kind", ["none", "rms", "layer"])
+@pytest.mark.parametrize("d,dtype", [(64, BF), (128, FP)])
+@pytest.mark.parametrize("T", [1, 7, 3000])
+def test_norms_of_rows_that_are_not_finite(kind, d, dtype, T):
+    """A head with an infinity or a NaN is NaN after a norm, is marked by its scale in the 8-bit cache with zeros for
+    codes, and leaves its neighbours (other heads of the token, other tokens) the bits that they have without it."""
+    hq, hkv = 6, 3
+    dims = vpb.attn_dims(hq, hkv, d, dtype=dtype)
+    x = _randn(4, T, hq + 2 * hkv, d, dtype=dtype)
+    gain = 1 + 0.2 * _randn(5, d, dtype=torch.float32)
+    hn = vpb.head_norm(kind, 1e-6, q_gain=gain, k_gain=gain) if kind != "none" else None
+    rope, pos = vpb.rope_axes(vpb.rope_axes_turns([d // 4, d // 4]).cuda()), torch.arange(2 * T, dtype=torch.int32, device="cuda")
+    bad = torch.zeros(T, hq + 2 * hkv, dtype=torch.bool, device="cuda")
+    bad[0, 1] = bad[T // 2, hq + 1] = bad[T - 1, hq + hkv + 2] = bad[T // 3, hq - 1] = bad[T // 3, hq + hkv - 1] = True
+
+    def store(t):
+        c = Cache8(9, [T], hkv, d, 64)
+        q, k = torch.zeros(T, hq, d, dtype=dtype, device="cuda"), torch.zeros(T, hkv, d, dtype=dtype, device="cuda")
+        vpb.vp_norm_rope_append(dims, hn, rope, t[:, :hq], t[:, hq:hq + hkv], t[:, hq + hkv:], _cu([T]), c.kv_len,
+                                pos, c.kv, q_out=q, k_out=k)
+        pg, row = c.at(0, 0, T)
+        codes, scales = torch.cat((c.k[pg, :, row], c.v[pg, :, row]), 1), torch.cat((c.ks[pg, :, row], c.vs[pg, :, row]), 1)
+        return torch.cat((q, k), 1), codes, scales
+
+    ref = store(x)
+    for value in (math.nan, math.inf, -math.inf):
+        t = x.clone()
+        t[..., 2] = torch.where(bad, torch.full_like(t[..., 2], value), t[..., 2])
+        rows, codes, scales = store(t)
+        lost, lost8 = bad[:, :hq + hkv], bad[:, hq:]
+        assert torch.equal(rows[~lost], ref[0][~lost])
+        if kind == "rms" and math.isinf(value):  # what is finite over an infinite root is 0
+            pair = torch.arange(d, device="cuda") % (d // 2) == 2
+            assert rows[lost][:, pair].isnan().all() and (rows[lost][:, ~pair] == 0).all()
+        else:
+            hit = ~rows[lost].isfinite()
+            assert hit.all() if kind != "none" else hit.any(-1).all()
+        assert torch.equal(codes[~lost8], ref[1][~lost8]) and torch.equal(scales[~lost8], ref[2][~lost8])
+        assert (codes[lost8] == 0).all() and (scales[lost8] == 255).all()
+
+
 # ------------------------------------------------------------------------------ factors of scores
 @pytest.mark.parametrize("n,hq,kernel", SHAPES)
 @pytest.mark.parametrize("d", [64, 128])
@@ -100,3 +180,44 @@ def test_scores_of_zero_under_the_largest_scales(n, hq, kernel, d, dtype, size, 
     out, lse = _run(q, k, v, dtype, scale, kernel, block=0)
     want, _, tol = _tolerance(q[:1], k, v, np.full(1, L), 1.0, dtype)
     assert np.all(np.abs(out - want[:, :1]) <= tol[:, :1]) and np.all(np.abs(lse - math.log(L)) <= 4e-5 + 4e-6 * math.log(L))
+
+
+# ------------------------------------------------------------------------------ scales of v
+@pytest.mark.parametrize("n,hq,kernel", SHAPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype,which", [(BF, "smallest"), (BF, "subnormal"), (BF, "largest"), (FP, "smallest"),
+                                         (FP, "largest")])
+def test_values_at_the_ends_of_the_range(n, hq, kernel, d, dtype, which):
+    """Values of one sign under the smallest and the largest scale, with the weight on them and rows of other sizes
+    beside them: the output is theirs.  An output of zero, or with a scale a power of two off, would exceed the
+    tolerance."""
+    rng = np.random.default_rng(d)
+    L = 900
+    heavy = np.arange(L) % 4 == 1
+    q, k = np.zeros((n, hq, d)), np.zeros((L, 1, d))
+    q[..., 0] = 1
+    k[:, 0, 0] = np.where(heavy, 40.0, 0.0)
+    ends = {"smallest": (rng.integers(8, 15, (L, 1, d)) * 2.0 ** rng.integers(0, 6, (L, 1, d)), 2.0 ** -14),
+            "subnormal": (rng.integers(1, 8, (L, 1, d)) * 2.0 ** -9, 2.0 ** -14),
+            "largest": (rng.integers(8, 15, (L, 1, d)) * 32.0, 2.0 ** 7)}[which]
+    v = np.where(heavy[:, None, None], ends[0] * ends[1], so.dequantise_rows(*so.quantise_rows(rng.standard_normal((L, 1, d)))))
+    scales = so.quantise_rows(v)[1][heavy]
+    assert np.all(scales == (134 if which == "largest" else 113))
+    out, _ = _run(q, k, v, dtype, 1.0, kernel, block=0)
+    want, _, tol = _tolerance(q[:1], k, v, np.full(1, L), 1.0, dtype)
+    assert np.all(want > 0) and np.all(tol < want / 4)
+    assert np.all(np.abs(out - want[:, :1]) <= tol[:, :1])
+
+
+@pytest.mark.parametrize("n,L,hq,kernel", [(1, 30011, 8, "rows"), (3, 12345, 4, "rows"), (200, 9001, 8, "tiles")])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_long_contexts_to_the_last_bits_of_the_weights(n, L, hq, kernel, d, dtype):
+    """Unit normal q, k and v over many keys (weights from 1 down to 2^-32 of the largest and below)."""
+    k, v = _exact(7, L, d), _exact(8, L, d)
+    q = _f64(_randn(9, n, hq, d, dtype=dtype))
+    out, lse = _run(q, k, v, dtype, 0.35, kernel)
+    rows = sorted({0, n // 2, n - 1})
+    want, want_lse, tol = _tolerance(q[rows], k, v, so.row_limits(n, L, 1)[rows], 0.35, dtype)
+    assert np.all(np.abs(out[rows] - want) <= tol)
+    assert np.all(np.abs(lse[rows] - want_lse) <= 4e-5 + 4e-6 * np.abs(want_lse))
