@@ -544,8 +544,14 @@ vp_status vp_read_cache8(const vp_attn_dims* dims, int32_t T, int32_t B, const v
 
 /*
  * vp_paged_attention8 -- vp_paged_attention over the 8-bit cache: the same mask, outputs and workspace,
- * over the values that the cache stands for, which are those that vp_read_cache8 gives back.  The weights are
- * rounded to 11 bits (fp16) for both types.  Of a page id outside the pool the keys and values are 0.
+ * over the values that the cache stands for, which are those that vp_read_cache8 gives back.  The products are of
+ * fp16 numbers for both types:
+ *   weights  rounded to 11 bits, those below 2^-21 of a row's largest to multiples of 2^-31 of it at most
+ *            (in out; the log-sum has them in 32 bits)
+ *   bf16 q   a row (token, head) times a power of two of its own: channels keep their 8 bits down to 2^-31 of the
+ *            row's largest magnitude, and below that are rounded to multiples of 2^-38 of the power of two at or
+ *            below it, where vp_paged_attention keeps them
+ * Of a page id outside the pool the keys and values are 0.
  */
 vp_status vp_paged_attention8(const vp_attn_dims* dims, int32_t T, int32_t B, const void* q,
                               int64_t q_stride, const int32_t* cu, const int32_t* kv_len,

@@ -360,8 +360,9 @@ __device__ __forceinline__ uint32_t to_codes(float x0, float x1, float x2, float
 }
 
 // A bf16 row of Q as fp16, the type of the products over the 8-bit cache: times a power of two that brings
-// its largest value to 2^14 .. 2^15, so that what lies within 2^-29 of it keeps its 8 bits (and the rest is at
-// most 2^-39 of it off).  top: the largest magnitude as fp32 bits; an infinity or a NaN becomes one.
+// its largest value to 2^14 .. 2^15, so that what lies within 2^-31 of it keeps its 8 bits, and the rest is at
+// most 2^-39 of it off (a score by 2^-39 max |q| sum |k|, where its 32-bit sum may be 2^-24 sum |q k| off).
+// top: the largest magnitude as fp32 bits; an infinity or a NaN stays one.
 struct HalfRow {
   float up, back;  // scores are multiplied by `back`
   __device__ __forceinline__ explicit HalfRow(uint32_t top) {

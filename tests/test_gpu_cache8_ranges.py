@@ -1,6 +1,6 @@
 """The 8-bit cache's operators at the ends of their number ranges, against the 64-bit definitions (oracle.streaming):
-infinities and NaN in q and under a norm, factors of scores whose products leave 32 bits, values at the smallest and
-largest scales.
+infinities and NaN in q and under a norm, factors of scores whose products leave 32 bits, channels of one row of q far
+apart, values at the smallest and largest scales.
 
 Tolerances of attention, where test_gpu_cache8.py allows more than a key can be off.  Weights are fp16 numbers,
 the row's largest at least 2^7 (the reference point lies 2^7 below the running maximum, or lower), so a weight p
@@ -180,6 +180,31 @@ def test_scores_of_zero_under_the_largest_scales(n, hq, kernel, d, dtype, size, 
     out, lse = _run(q, k, v, dtype, scale, kernel, block=0)
     want, _, tol = _tolerance(q[:1], k, v, np.full(1, L), 1.0, dtype)
     assert np.all(np.abs(out - want[:, :1]) <= tol[:, :1]) and np.all(np.abs(lse - math.log(L)) <= 4e-5 + 4e-6 * math.log(L))
+
+
+# ------------------------------------------------------------------------------ channels of q far apart
+@pytest.mark.parametrize("n,hq,kernel", SHAPES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_channels_of_q_far_apart(n, hq, kernel, d):
+    """A bf16 row of q keeps its 8 bits down to 2^-31 of its largest magnitude, and below that the multiples of 2^-38
+    of the power of two at or below it (halves to even): the weights are those of that row."""
+    rng = np.random.default_rng(n)
+    L = 1200
+    small = rng.integers(128, 256, (n, hq, d)) / 128 * rng.choice([-1, 1], (n, hq, d)) * 2.0 ** rng.integers(-3, 3, (n, hq, d))
+    for power in (20, 28, 33, 38, 42, 60):
+        q = small.copy()
+        q[..., 0] = 1.5 * 2.0 ** power                     # over a channel of k that is 0
+        unit = 2.0 ** (power - 38)
+        held = np.where(np.abs(q) < 2.0 ** (power - 28), np.round(q / unit) * unit, q)
+        assert power > 30 or np.array_equal(held, q)
+        k = np.zeros((L, 1, d))
+        k[:, 0, 1:9] = rng.integers(-7, 8, (L, 8)) / 4
+        v = _exact(6, L, d)
+        out, lse = _run(q, k, v, BF, 0.25, kernel, block=0)
+        rows = sorted({0, n // 2, n - 1})
+        want, want_lse, tol = _tolerance(held[rows], k, v, np.full(len(rows), L), 0.25, BF)
+        assert np.all(np.abs(out[rows] - want) <= tol)
+        assert np.all(np.abs(lse[rows] - want_lse) <= 4e-5 + 4e-6 * np.abs(want_lse))
 
 
 # ------------------------------------------------------------------------------ scales of v
