@@ -444,7 +444,8 @@ typedef struct vp_rope_axes {
 /* Paged cache in 8 bits.  A row (one token, one kv head) is d e4m3 codes and a scale 2^e as the byte
    e + 127 (e8m0): value = code x 2^e.  vp_norm_rope_append takes the least e with max |x| <= 448 x 2^e, held
    to [-14, 7], and rounds x / 2^e to the nearest code (ties to even): 4 significant bits for
-   values down to 2^-13 of the row's largest, and every value is a bf16 and an fp16 number.  Values beyond
+   values down to 2^-13 of the row's largest or 2^-20, whichever is larger; smaller ones are off by at most 2^-17 of
+   the row's largest or 2^-24, whichever is larger.  Every value is a bf16 and an fp16 number.  Values beyond
    57,344 are held there, those up to 2^-24 vanish.  A row with an infinity or a NaN gets the byte 255 and reads
    as NaN; so does any other byte outside 113 .. 134, and a code 0x7F or 0xFF.
    Pages and rows lie as in vp_paged_kv; k, v and the scales are 16-byte aligned. */

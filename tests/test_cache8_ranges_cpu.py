@@ -1,5 +1,5 @@
 """That the tolerances of test_gpu_cache8_ranges.py see the mistakes they are there for (planted in the results of
-the 64-bit definition)."""
+the 64-bit definition), and what the 8-bit cache's rows keep of their values, by the definition."""
 import numpy as np
 import pytest
 
@@ -34,3 +34,20 @@ def test_tolerances_see_a_lost_tile_of_keys(L):
     p = np.exp(0.35 * (q[0, 0] @ k[:, 0].T) - lse[0, 0])
     p[np.argsort(p)[-64:-32]] = 0
     assert np.any(np.abs(p @ v[:, 0] - want[0, 0]) > tol[0, 0])
+
+
+def test_what_a_row_keeps():
+    """4 significant bits (half a step: 2^-4) down to 2^-13 of the row's largest or 2^-20, below that at most 2^-17 of the
+    largest or 2^-24: rows of all sizes, those whose exponent is held at -14 among them, each with values far apart."""
+    rng = np.random.default_rng(0)
+    top = 2.0 ** rng.uniform(-26, 15.8, (4000, 1))
+    x = top * 2.0 ** -rng.uniform(0, 24, (4000, 64)) * rng.choice([-1, 1], (4000, 64))
+    m = np.abs(x).max(-1, keepdims=True)
+    assert (m <= 57344).all() and (m < 2.0 ** -20).any()
+    codes, scales = so.quantise_rows(x)
+    off = np.abs(so.dequantise_rows(codes, scales) - x)
+    whole = np.abs(x) >= np.maximum(2.0 ** -13 * m, 2.0 ** -20)
+    assert whole.any() and np.all(off[whole] <= 2.0 ** -4 * np.abs(x[whole]))
+    assert np.all(off <= np.where(whole, np.inf, np.maximum(2.0 ** -17 * m, 2.0 ** -24)))
+    held = (scales == 113)[:, None]
+    assert np.any(off > 2.0 ** -4 * np.abs(x), axis=-1, where=held).sum() > 100  # rows with fewer bits for some
