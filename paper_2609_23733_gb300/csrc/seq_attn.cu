@@ -213,7 +213,8 @@ struct TileSmem {
   uint16_t k[C::kStages][C::kHalves][C::kBN * 64];
   uint16_t v[C::kStages][C::kHalves][C::kBN * 64];
   uint64_t q_full[C::kChains], q_empty[C::kChains], q_half[C::kChains];
-  uint64_t k_full[C::kStages], v_full[C::kStages], k_empty[C::kStages], v_empty[C::kStages];
+  uint64_t k_full[C::kStages], v_full[C::kStages], v_empty[C::kStages];
+  uint64_t k_empty[C::kAlias ? C::kStages : 1];  // 128-key tiles; 64-key ones are released as a whole, by v_empty
   uint64_t s_full[C::kChains], s_empty[C::kChains], p_full[C::kChains], o_bar[C::kChains],
       o_empty[C::kChains], drain[C::kChains], turn[C::kChains];
   uint32_t tmem_base;
@@ -660,7 +661,7 @@ __global__ void __launch_bounds__(Cfg<D, kKeys == Keys::paged8>::kThreads, 1)
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&sm.k_full[s], k8 ? C::kFill : 1);
       mbar_init(&sm.v_full[s], k8 ? C::kFill : 1);
-      mbar_init(&sm.k_empty[s], kChains);
+      if (kAlias) mbar_init(&sm.k_empty[s], kChains);  // (64-key tiles: v_empty stands for both)
       mbar_init(&sm.v_empty[s], kChains);
     }
     for (int c = 0; c < kChains; ++c) {
