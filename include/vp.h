@@ -414,7 +414,8 @@ typedef struct vp_rope_options {
 /* Norm of the heads of q and of k over their d channels, ahead of the rotation, in 32 bits:
      RMS:    y = x / sqrt(mean(x^2) + eps) (.) g + b
      LAYER:  y = (x - mean(x)) / sqrt(var(x) + eps) (.) g + b      (biased variance; qk-norm)
-   A gain or bias that is NULL is 1 or 0.  Gains and biases are [d], shared by the heads, or [heads][d]. */
+   A gain or bias that is NULL is 1 or 0.  Gains and biases are [d], shared by the heads, or [heads][d].  A head whose
+   sum of squares passes 32 bits (bf16 magnitudes of 2^60 and more) is divided by infinity: y = b. */
 #define VP_NORM_NONE 0
 #define VP_NORM_RMS 1
 #define VP_NORM_LAYER 2

@@ -142,6 +142,23 @@ def test_norms_of_rows_that_are_not_finite(kind, d, dtype, T):
         assert (codes[lost8] == 0).all() and (scales[lost8] == 255).all()
 
 
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_norms_of_heads_whose_squares_pass_32_bits(kind, d):
+    x = _randn(1, 3, 4, d, dtype=BF)
+    x[1, 2] *= 2.0 ** 80
+    x[2, :] *= 2.0 ** 50  # squares of 2^100: in range
+    gain, bias = (_randn(s, d, dtype=torch.float32) for s in (2, 3))
+    out = torch.empty_like(x)
+    rope = vpb.rope_axes(torch.zeros(1, 0, dtype=torch.int64, device="cuda"))
+    vpb.vp_norm_rope_append(vpb.attn_dims(4, 4, d), vpb.head_norm(kind, 1e-6, k_gain=gain, k_bias=bias), rope, None, x, None,
+                            _cu([3]), None, None, None, k_out=out)
+    want = so.head_norm(_f64(x), kind, 1e-6, _f64(gain), _f64(bias))
+    want[1, 2] = _f64(bias)
+    err = 2.0 ** -15 * np.abs(want).max(-1, keepdims=True)  # test_gpu_cache8.py: 32-bit norms
+    assert np.all(np.abs(_f64(out) - want) <= err + EPS[BF] * np.abs(want))
+
+
 # ------------------------------------------------------------------------------ factors of scores
 @pytest.mark.parametrize("n,hq,kernel", SHAPES)
 @pytest.mark.parametrize("d", [64, 128])
