@@ -29,9 +29,10 @@
 // tile (d 128: half a tile) ahead, and write them as fp16 tiles (Filler); Q of bf16 is brought to fp16 in shared memory by the softmax
 // warps, a row per thread.  2 chunks of about 4,000 tokens over 30,000 keys, 16 heads of 128 on 4 kv heads: 1.43 ms
 // as called (1,360 TFLOP/s; the 16-bit cache 1.39-1.46 ms under the power limit); a view of 1,374 tokens over
-// 43,968 keys, 16 heads of 64 on 4: 258 us, 268 with the cache not in L2 (the 16-bit cache 204-212): 5 warps a
-// scheduler instead of 4, and the unpacking's instructions (9 % of the time) lengthen the chains' steps.  Slower: codes by TMA into a ring of their own
-// and unpacked from there (d 64: 318, and the fp16 ring then has half the stages; d 128 1.74 ms), by cp.async
+// 43,968 keys, 16 heads of 64 on 4: 258 us, 268 with the cache not in L2 (the 16-bit cache 203).  Of the difference 32 us
+// come before any unpacking (235 us with a ring that nobody fills: 5 warps a scheduler instead of 4, which poll; 128
+// registers a softmax thread instead of 152), 7 with the unpacking of codes that are not read (242), 15 with their loads.
+// Slower: codes by TMA into a ring of their own and unpacked from there (d 64: 318, and the fp16 ring then has half the stages; d 128 1.74 ms), by cp.async
 // (334, 2.08 ms), the unpacking warps waiting at a barrier instead of polling (334 against 310).
 // A chain stops at its own last visible key; the tiles after it are only released.  A tile that
 // some row of the chain does not see in full takes the masked path: scores past a row's limit
@@ -1438,10 +1439,12 @@ namespace {
 //     64, 1 x 2,048: 9.3 / 22    64, 16 x 4,096: 30 / 36    64, 16 x 4,096, 16 kv heads: 137 / 89
 //     128, 1 x 32,768: 28 / 28   128, 16 x 4,096: 51 / 36   128, 4 x 8,192, 2 kv heads of 128: 25 / 36
 //   8-bit cache (on the device)
-//     8, 16 x 4,096, 16 kv heads: 34 / 133   32, 64 x 4,096: 64 / 134   64, 1 x 2,048: 10.1 / 23
-//     64, 16 x 4,096: 37 / 37    128, 1 x 32,768: 34 / 31   128, 16 x 4,096: 62 / 36   256, 1 x 2,048: 12.9 / 30
-//     256, 1 x 8,192: 22 / 37    64, 16 x 4,096, 16 kv heads: 115 / 136   128, 4 x 8,192, 2 kv heads of 128: 30 / 43
-//     160, 25 x 389 and fewer, 4 kv heads of 128: 43 / 21 (1,000 items: starting one costs more than its few keys)
+//     8, 16 x 4,096, 16 kv heads: 33 / 152   32, 64 x 4,096: 65 / 156   64, 1 x 2,048: 10.1 / 23
+//     64, 16 x 4,096: 38 / 37    128, 1 x 32,768: 34 / 31   128, 16 x 4,096: 63 / 36   256, 1 x 2,048: 12.9 / 30
+//     256, 1 x 8,192: 22 / 37    64, 16 x 4,096, 16 kv heads: 116 / 157   128, 4 x 8,192, 2 kv heads of 128: 30 / 43
+//     160, 25 x 389 and fewer, 4 kv heads of 128: 39 / 22 (1,000 items: starting one costs more than its few keys)
+//   It keeps the 16-bit cache's bounds of 128 rows and 20,000 units, which miss two of these lines: 64 rows on 16 kv
+//   heads (and 64 sequences of them on 4: 116 / 156) go to the tiles, 128 rows over 32,768 keys to few rows.
 //   prompts x tokens, 16 kv heads
 //     1 x 256: 8.4 / 10.8   1 x 400: 11.1 / 12.4   1 x 512: 19.2 / 13.3   8 x 64: 8.4 / 10.3
 //     8 x 128: 15.1 / 13.9  64 x 16: 13.1 / 39.4   64 x 64: 29 / 39 (4 kv heads: 29 / 17)
